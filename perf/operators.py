@@ -124,6 +124,11 @@ def _layer(case, seed):
     return {"lut_k": signposts(), "lut_v": signposts(), "s": s, "z": z, "lo": lo, "hi": hi}
 
 
+def _pointers(B, cap):
+    """Zeros [B, cap + 1], each row 16-byte aligned as the library's caches are."""
+    return torch.zeros(B, cap + 4, dtype=torch.int32, device=DEV)[:, :cap + 1]
+
+
 def _strata(case):
     return max(1, int(math.ceil(case["outliers"] * case["kv_heads"] * 128))) if case["outliers"] > 0 else 0
 
@@ -152,7 +157,7 @@ def _outliers(g, case, lens, cap, scales, thin):
     """ptr [B, cap + 1], idx and val [B, entries]: one channel of each of n equal strata of a token, some left out."""
     B, D, n = len(lens), case["kv_heads"] * 128, _strata(case)
     room = max(8, n * cap)
-    ptr = torch.zeros(B, cap + 1, dtype=torch.int32, device=DEV)
+    ptr = _pointers(B, cap)
     idx = torch.zeros(B, room, dtype=torch.int16, device=DEV)
     val = torch.zeros(B, room, dtype=torch.int16, device=DEV)
     for i in range(B if n else 0):
@@ -189,7 +194,7 @@ def _empty(case, B, cap):
     z = lambda m, t: torch.zeros(B, m, dtype=t, device=DEV)  # noqa: E731
     room = max(8, n * cap)
     return {"k_codes": z(cap * H * 16 * b, torch.uint8), "v_codes": z(cap * H * 16 * b, torch.uint8), "v_sz": z(2 * cap, torch.int16),
-            "k_ptr": z(cap + 1, torch.int32), "v_ptr": z(cap + 1, torch.int32), "k_idx": z(room, torch.int16),
+            "k_ptr": _pointers(B, cap), "v_ptr": _pointers(B, cap), "k_idx": z(room, torch.int16),
             "k_val": z(room, torch.int16), "v_idx": z(room, torch.int16), "v_val": z(room, torch.int16)}
 
 
