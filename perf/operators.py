@@ -338,6 +338,16 @@ def _values(case, s, layer, cap, sink):
     return v.view(-1, cap, H, 128).transpose(1, 2).contiguous()
 
 
+def _long_product(y, v, n=8192):
+    """y @ v, [H, M, T] by [H, T, 128], summed n tokens at a time: one 32-bit sum over half a million is 2e-5 off."""
+    H, M, T = y.shape
+    if T <= n:
+        return y @ v
+    k = (T + n - 1) // n
+    y = torch.nn.functional.pad(y, (0, k * n - T)).view(H, M, k, n).transpose(1, 2).contiguous()
+    return (y @ torch.nn.functional.pad(v, (0, 0, 0, k * n - T)).view(H, k, n, 128)).sum(1)
+
+
 def _attend_plain(s):
     case, layer = s["case"], s["layer"]
     B, H, R, P = case["seqs"], case["kv_heads"], case["q_heads"] // case["kv_heads"], case["prefix"]
@@ -353,7 +363,7 @@ def _attend_plain(s):
         my = y.max(-1, keepdim=True)[0]
         m = torch.maximum(m, my.view(H, B, R, 1).permute(1, 0, 2, 3))
         y = torch.exp(y - m.permute(1, 0, 2, 3).reshape(H, B * R, 1))
-        o2 = (y @ _values(case, s["prefix"], layer, _up(P), s["sink"])[0, :, :P]).view(H, B, R, 128).permute(1, 0, 2, 3)
+        o2 = _long_product(y, _values(case, s["prefix"], layer, _up(P), s["sink"])[0, :, :P]).view(H, B, R, 128).permute(1, 0, 2, 3)
         l2 = y.sum(-1).view(H, B, R, 1).permute(1, 0, 2, 3)
     m = torch.where(m == -math.inf, 0.0, m)
     x = torch.exp(x - m)
