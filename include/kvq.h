@@ -293,6 +293,66 @@ int32_t kvq_decode_step_launches(const kvq_cache *cache);
 kvq_status kvq_attention_decode_noalloc(const kvq_cache *cache, const float *d_q_rot, float scale,
                                         float *d_scores, int64_t ld_scores, float *d_out, void *stream);
 
+/*
+ * One decode step's attention for a batch of sequences of one layer that may share a prefix (paper Sec. 3: generation-time
+ * attention over the quantized cache, here for n_seqs queries at once):
+ *   out[b][q][c] = sum_n softmax_n(x[b][q][.])[n] * vhat[n][kv(q)*128 + c],
+ *   x[b][q][n] = scale * sum_c q_rot[b][q][c] * RoPE_n(khat[n][kv(q)])[c],
+ * n over the tokens of `prefix` (positions 0 .. P-1) and then those of caches[b] (its token j at position P + j), khat and
+ * vhat as defined for kvq_qk_matvec and kvq_pv_matvec.  The prefix is read, de-quantised and rotated once for 64 queries
+ * of a KV head at a time, whatever sequences they belong to.
+ *   prefix   : the shared tokens, or NULL (a batch of unrelated sequences; P = 0).
+ *   caches   : HOST array of n_seqs caches, or NULL (no sequence has tokens of its own); a NULL entry is a sequence without
+ *              tokens of its own.  The same cache may be listed more than once, and `prefix` among them: nothing is written
+ *              to any of them, their own workspaces included.  At least one cache of the call must be given.
+ *   All caches of a call have the same bits, n_kv_heads, n_q_heads and rope_base, are loaded (each uses its own constants)
+ *   and have n_tokens_k == n_tokens_v; any of them may be empty, use blocked outlier storage, or keep attention-sink tokens.
+ *   n_q_heads / n_kv_heads may be any whole number.
+ *   d_q_rot  : DEVICE fp32 [n_seqs][n_q_heads][128], each rotated to its sequence's position (P + own tokens - 1, as a rule).
+ *   d_out    : DEVICE fp32 [n_seqs][n_q_heads][128]; zero for a sequence without any tokens.
+ *   d_workspace : DEVICE, 16-byte aligned, kvq_attention_decode_batch_workspace_bytes() bytes for the same arguments and token
+ *              counts (0: the arguments are not usable).  It grows with the tokens: 4 bytes per outlier entry above all.
+ * The matrix products take fp16 factors in two parts with fp32 sums: results agree with kvq_attention_decode on the joined
+ * sequence to fp32 rounding, and are run-to-run identical.  The descriptors are read during the call: token counts are those
+ * of the call, also where it is captured into a graph.  Calls that share a workspace must not overlap.
+ * Errors: INVALID_ARG, UNSUPPORTED, NOT_LOADED, CAPACITY (workspace), HIP.
+ */
+int64_t kvq_attention_decode_batch_workspace_bytes(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs);
+kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs,
+                                      const float *d_q_rot, float scale, float *d_out, void *d_workspace,
+                                      int64_t workspace_bytes, void *stream);
+
+/*
+ * Tokens from cache to cache.  Keys are stored before the rotation and a token's position is its index, so tokens may land
+ * at any place with their codes, scales and outliers as they are stored: nothing is quantized again, and results of the
+ * appends, mat-vecs and fused calls on the destination are those of a cache to which the same tokens had been appended.
+ *
+ * kvq_cache_copy: for every i < n_copies, tokens first[i] .. first[i] + count[i] - 1 of src[i] are appended to dst[i] (a fork:
+ * all tokens to an empty cache; beam search: each hypothesis takes over its parent's tokens; a continuation behind a shared
+ * prefix: the tokens from some place on).  count[i] = 0 is allowed.  The same source may be listed more than once; a
+ * destination may not, nor be a source of the same call (INVALID_ARG, also by its code buffers' addresses).
+ * kvq_cache_gather: tokens d_tokens[0 .. n-1] of src, in that order, are appended to dst (compaction: the tokens that an
+ * eviction keeps).  Any order, repeats allowed; d_tokens: DEVICE int32.  An index outside the source's tokens sets dst's
+ * *d_status to KVQ_ERR_INVALID_ARG and appends a token of unspecified finite content.  Uses dst->workspace (8 bytes per 256 listed
+ * tokens: covered by kvq_workspace_bytes).
+ * kvq_cache_truncate: the tokens from n_tokens on are dropped (a rejected draft, an abandoned branch); their storage is free for
+ * the next tokens.  Host only, no stream: nothing needs clearing, appends and copies overwrite.
+ *
+ * Both caches of a pair have the same bits, n_kv_heads and rope_base; all destinations of one copy the same bits and
+ * n_kv_heads.  Capacities, outlier storage (flat or blocked), k_side_v and n_q_heads may differ.  The destination has
+ * n_tokens_k == n_tokens_v (they advance together); a source needs the copied tokens on both sides, for a gather also
+ * n_tokens_k == n_tokens_v.  The constants of kvq_lut_load: a destination that has not been loaded must be empty and takes over the
+ * source's (params is copied on `stream`, loaded is set); one that has been keeps its own, which are the caller's to be the
+ * same.  Attention-sink tokens: a token that lands below dst->n_sink must be one of the source's (its fp16 row is copied;
+ * INVALID_ARG otherwise, for a gather through *d_status, with a zero row); one that lands elsewhere goes on with its codes.
+ * Outliers that do not fit dst's capacity are dropped and *d_status is set as for the appends.  All host checks come before
+ * the first launch.  Errors: INVALID_ARG, UNSUPPORTED, NOT_LOADED, CAPACITY (tokens, workspace), HIP.
+ */
+kvq_status kvq_cache_copy(kvq_cache *const *dst, const kvq_cache *const *src, const int64_t *first, const int64_t *count,
+                          int32_t n_copies, void *stream);
+kvq_status kvq_cache_gather(kvq_cache *dst, const kvq_cache *src, const int32_t *d_tokens, int64_t n, void *stream);
+kvq_status kvq_cache_truncate(kvq_cache *cache, int64_t n_tokens);
+
 /* ---- helpers beyond the calls above ------------------------------------------------------- */
 
 /*

@@ -65,6 +65,11 @@ def load_library():
         "kvq_pv_matvec": (C.c_int, [P, V, I64, V, V]),
         "kvq_attention_decode": (C.c_int, [P, V, F, V, I64, V, V]),
         "kvq_attention_decode_noalloc": (C.c_int, [P, V, F, V, I64, V, V]),
+        "kvq_attention_decode_batch_workspace_bytes": (I64, [P, V, I32]),
+        "kvq_attention_decode_batch": (C.c_int, [P, V, I32, V, F, V, V, I64, V]),
+        "kvq_cache_copy": (C.c_int, [V, V, V, V, I32, V]),
+        "kvq_cache_gather": (C.c_int, [P, P, V, I64, V]),
+        "kvq_cache_truncate": (C.c_int, [P, I64]),
         "kvq_decode_step": (C.c_int, [P, V, V, V, F, V, I64, V, V]),
         "kvq_decode_step_launches": (I32, [P]),
         "kvq_softmax_workspace_bytes": (I64, [I32, I64]),
@@ -108,6 +113,8 @@ EXPORTED_SYMBOLS = [
     "kvq_profile_span_buffer_bytes", "kvq_profile_set_span_buffer", "kvq_profile_span_us", "kvq_calibrate_workspace_bytes", "kvq_calibrate_nuq",
     "kvq_calibrate_key_channels", "kvq_calibrate_key_channels_workspace_bytes", "kvq_calibrate_key_channels_ws",
     "kvq_stream_read_workspace_bytes", "kvq_stream_read",
+    "kvq_attention_decode_batch", "kvq_attention_decode_batch_workspace_bytes",
+    "kvq_cache_copy", "kvq_cache_gather", "kvq_cache_truncate",
 ]
 
 
@@ -334,6 +341,23 @@ class KvqCache:
             torch.cuda.synchronize(self.device)                 # the old arrays are released after the copies
         return grew
 
+    def free_nnz_blocks(self) -> int:
+        """Blocked storage: gives back the blocks behind the entries in use (after kvq_cache_truncate), keeping one per array.
+        Returns how many blocks.  Synchronises, since work that reads them may be under way."""
+        if not self.block_entries:
+            return 0
+        freed = 0
+        used = self.nnz_used()
+        torch.cuda.synchronize(self.device)
+        for n, cap_name, names in ((used[0], "cap_nnz_k", ("k_idx", "k_val")), (used[1], "cap_nnz_v", ("v_idx", "v_val"))):
+            keep = max(1, -(-n // self.block_entries))
+            for name in names:
+                freed += max(0, len(self.blocks[name]) - keep)
+                del self.blocks[name][keep:]
+                self.tables[name][keep:] = 0
+            setattr(self.c, cap_name, min(getattr(self.c, cap_name), keep * self.block_entries))
+        return freed
+
 
 def _host_u16(a):
     a = np.ascontiguousarray(a)
@@ -435,6 +459,70 @@ def kvq_attention_decode_noalloc(cache: KvqCache, q_rot: torch.Tensor, scale: fl
     _check(load_library().kvq_attention_decode_noalloc(C.byref(cache.c), q_rot.data_ptr(), float(scale),
                                                        scores.data_ptr(), scores.stride(0), out.data_ptr(),
                                                        _stream_ptr(stream)), "kvq_attention_decode_noalloc")
+
+
+def _cache_array(caches):
+    """Host array of descriptor pointers (None: a null entry)."""
+    return (C.c_void_p * len(caches))(*[None if c is None else C.addressof(c.c) for c in caches])
+
+
+def kvq_attention_decode_batch_workspace_bytes(prefix, caches, n_seqs: int) -> int:
+    """Workspace of a kvq_attention_decode_batch call with these arguments; 0 if they are not usable."""
+    assert caches is None or len(caches) == n_seqs
+    return int(load_library().kvq_attention_decode_batch_workspace_bytes(
+        None if prefix is None else C.byref(prefix.c), None if caches is None else _cache_array(caches), n_seqs))
+
+
+def kvq_attention_decode_batch(prefix, caches, q_rot: torch.Tensor, scale: float, out: torch.Tensor, workspace: torch.Tensor = None,
+                               stream=None):
+    """Attention of one decode step for q_rot.shape[0] sequences: the tokens of `prefix` (a KvqCache or None), then those of
+    caches[b] (a list of KvqCache or None, or None).  workspace: uint8 tensor, allocated here if None."""
+    assert q_rot.is_cuda and q_rot.dtype == torch.float32 and q_rot.dim() == 3 and q_rot.is_contiguous()
+    n_seqs = q_rot.shape[0]
+    assert caches is None or len(caches) == n_seqs
+    some = [c for c in ([prefix] if prefix is not None else []) + list(caches or []) if c is not None]
+    assert some and all(q_rot.shape[1:] == (c.c.n_q_heads, 128) and c.device == q_rot.device for c in some)
+    assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and out.shape == q_rot.shape
+    assert out.device == q_rot.device
+    lib = load_library()
+    pre = None if prefix is None else C.byref(prefix.c)
+    arr = None if caches is None else _cache_array(caches)
+    if workspace is None:
+        workspace = _scratch(int(lib.kvq_attention_decode_batch_workspace_bytes(pre, arr, n_seqs)) or 256, q_rot.device, stream)
+    assert workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.device == q_rot.device
+    _check(lib.kvq_attention_decode_batch(pre, arr, n_seqs, q_rot.data_ptr(), float(scale), out.data_ptr(), workspace.data_ptr(),
+                                          workspace.numel(), _stream_ptr(stream)), "kvq_attention_decode_batch")
+
+
+def kvq_cache_copy(dst, src, first=0, count=None, stream=None):
+    """Appends tokens first .. first + count - 1 of src to dst (count None: all from `first` on).  dst and src: a KvqCache each, or
+    lists of the same length (one launch for a dozen copies); first and count: a number for all, or a list."""
+    one = isinstance(dst, KvqCache)
+    ds, ss = ([dst], [src]) if one else (list(dst), list(src))
+    n = len(ds)
+    assert len(ss) == n and all(isinstance(c, KvqCache) for c in ds + ss)
+    assert all(d.device == s.device for d, s in zip(ds, ss))
+    f = [int(first)] * n if not isinstance(first, (list, tuple)) else [int(x) for x in first]
+    if count is None:
+        k = [s.n_tokens_k - x for s, x in zip(ss, f)]
+    else:
+        k = [int(count)] * n if not isinstance(count, (list, tuple)) else [int(x) for x in count]
+    assert len(f) == n and len(k) == n
+    _check(load_library().kvq_cache_copy(_cache_array(ds), _cache_array(ss), (C.c_int64 * n)(*f), (C.c_int64 * n)(*k), n,
+                                         _stream_ptr(stream)), "kvq_cache_copy")
+
+
+def kvq_cache_gather(dst: KvqCache, src: KvqCache, tokens: torch.Tensor, stream=None):
+    """Appends the listed tokens of src (int32, on the GPU) to dst, in that order."""
+    assert tokens.is_cuda and tokens.dtype == torch.int32 and tokens.dim() == 1 and tokens.is_contiguous()
+    assert dst.device == src.device == tokens.device
+    _check(load_library().kvq_cache_gather(C.byref(dst.c), C.byref(src.c), tokens.data_ptr(), tokens.numel(), _stream_ptr(stream)),
+           "kvq_cache_gather")
+
+
+def kvq_cache_truncate(cache: KvqCache, n_tokens: int):
+    """Drops the tokens from n_tokens on (host only)."""
+    _check(load_library().kvq_cache_truncate(C.byref(cache.c), int(n_tokens)), "kvq_cache_truncate")
 
 
 def kvq_softmax_f32(x: torch.Tensor, probs: torch.Tensor, n_cols: int, workspace: torch.Tensor, stream=None):

@@ -1,0 +1,891 @@
+// One decode step's attention for a batch of sequences that share a prefix (paper Sec. 3: generation-time attention over
+// the quantized cache; Sec. 3.2: Keys rotated after de-quantisation).
+//
+//   out[b][q] = sum_n softmax_n(x[b][q][.])[n] vhat[n],   x[b][q][n] = scale <q_rot[b][q], R_n khat[n]>,
+//
+// n over the prefix's tokens and the sequence's own, whose positions follow the prefix's.  A token's Key is de-quantised
+// and rotated once for all queries that see it, so the work per element no longer depends on the batch until the products
+// do: they run on the matrix cores, the only units with the rate for (tokens x queries x 128) twice.
+//
+// Numbers.  The products are fp16 with fp32 sums, yet as exact as fp32 ones: a factor that is not an fp16 number goes in as
+// two (x = hi + lo, 22 bits or 2^-24 absolute, whichever is coarser), lo * lo left out.
+//   scores  K' = R_n khat in two parts, the query in two parts (scaled by a power of two per query): three products.
+//   output  vhat = s_n lut[code] + z_n + residual.  lut[code] and the residuals are fp16 numbers as they are stored, so
+//           sum_n (p_n s_n) lut[code] + sum_n p_n (residual + z_n) needs only the weights in two parts: two products each.
+// Weights are scaled by 2^kappa, which keeps p_n and p_n s_n below 2^15 and the absolute error of the small ones at 2^-24 / 2^kappa.
+//
+// Layout.  A wavefront takes 32 tokens at a time.  Operands of v_mfma_f32_16x16x32_f16 hold eight k-indices per lane, and
+// a k-index may stand for any channel (any token) as long as both operands agree.  So a lane (token r, group g) de-quantises
+// the 16 channel pairs 16 g .. 16 g + 15 of its token, which are consecutive fields of its chunk, straight into operand
+// registers; the scores come out with a query per lane column and tokens 4 g .. 4 g + 3 in its registers, which is the
+// weights' operand of the second product as it stands; and the Values' operand, two tokens to a field, comes from one look-up
+// per field.  Nothing crosses lanes but the maximum of a query's 32 scores.
+//
+// Outliers reach their element through LDS: a first kernel sorts the entries of every 32 tokens by head, and the wavefront
+// scatters its head's residuals into a zeroed patch that it reads beside the codes.
+#include <math.h>
+#include <string.h>
+#include "kvq_common.hpp"
+#include "kvq_qk_sparse.hpp"
+
+namespace {
+
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+
+constexpr int BT_BLOCK = 32;            // tokens a wavefront takes at a time
+constexpr int BT_WAVES = 4;             // wavefronts of a workgroup
+constexpr int BT_NT = 64 * BT_WAVES;
+constexpr int BT_ROW = 256;             // halves of a query's row: 128 high parts, 128 low parts
+constexpr int BT_SEGS = 24;             // descriptors that travel in one launch's arguments
+constexpr int BT_MAX_HEADS = 512;
+constexpr int BT_PATCH = 8192;          // bytes of a wavefront's patch
+constexpr float BT_MAX_SLACK = 6.0f;    // the running maximum follows a larger score from 2^6 times the weight on
+constexpr int BT_KAPPA = 9;             // 2^(6 + 9) is the largest weight then
+
+// One cache as the kernels see it.
+struct BtSeg {
+    const uint8_t *k_codes, *v_codes;
+    const uint32_t *v_sz;               // fp16 scale, zero-point of a token
+    const uint32_t *k_ptr, *v_ptr;
+    const void *k_idx, *k_val, *v_idx, *v_val;     // flat arrays, or tables of blocks (shift != 0)
+    const void *params;
+    const uint16_t *sink_k, *sink_v;
+    int64_t k_list, v_list;             // places of its sorted entries
+    uint32_t k_room, v_room;
+    int32_t n, cap, shift, n_sink;
+    int32_t blk0;                       // number of its first 32-token block
+    int32_t chunk0;                     // number of its first workgroup's tokens among those of its launch
+};
+
+struct BtWork {                         // the workspace
+    BtSeg *segs;                        // [0] the prefix, [1 + b] sequence b's own
+    uint32_t *k_start, *v_start;        // [block][heads + 1]: first entry of a head
+    float *smax;                        // [block]: largest Value scale
+    _Float16 *rows[2];                  // query rows: for the prefix [head][b][r], for the own tokens [b][head][r]
+    float *row_scale[2];
+    uint32_t *k_list, *v_list;          // entries: residual << 16 | token << 7 | channel
+    float *part_o[2], *part_ml[2];      // [chunk][head][query] sums of a workgroup: output; maximum, weights
+};
+
+struct BtArgs {
+    BtWork w;
+    const float *q;
+    float *out;
+    float scale;
+    int32_t n_seqs, heads, ratio, prefix, own;     // own: some sequence has tokens of its own
+    int32_t chunk[2], n_chunks[2], mp[2];          // blocks per workgroup, workgroups per head, queries per slot (padded)
+};
+
+struct BtSegs {
+    BtSeg seg[BT_SEGS];
+    int32_t wg0[BT_SEGS + 1];                      // first workgroup of each
+    int32_t first, n;                              // number of the first, how many
+};
+
+static_assert(sizeof(BtArgs) + sizeof(BtSegs) + 16 <= 4096, "kernel arguments");
+
+template <bool BLOCKED>
+__device__ __forceinline__ uint32_t bt_entry(const void *arr, int shift, uint32_t e)
+{
+    if (!BLOCKED) return ((const uint16_t *)arr)[e];
+    return ((const uint16_t *const *)arr)[e >> shift][e & ((1u << shift) - 1u)];
+}
+
+// The entries of 32 tokens sorted by head: counted per head, then dealt out.  (Their order within a head is any: every entry
+// has an element of its own.)
+template <bool BLOCKED>
+__device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int n,
+                             int heads, uint32_t *start, uint32_t *list, uint32_t *count)
+{
+    const int tid = threadIdx.x, t = tid >> 3, l = tid & 7;
+    for (int h = tid; h < heads; h += BT_NT) count[h] = 0u;
+    uint32_t p0 = 0, p1 = 0;
+    if (n0 + t < n) {
+        p0 = ptr[n0 + t];
+        p1 = ptr[n0 + t + 1];
+        p1 = p1 < room ? p1 : room;
+    }
+    const uint32_t base = ptr[n0];
+    __syncthreads();
+    for (uint32_t e = p0 + l; e < p1; e += 8) {
+        const uint32_t h = bt_entry<BLOCKED>(idx, shift, e) >> 7;
+        if (h < (uint32_t)heads) atomicAdd(&count[h], 1u);
+    }
+    __syncthreads();
+    if (tid < 64) {                                 // exclusive sums, eight heads a lane
+        uint32_t c[BT_MAX_HEADS / 64], s = 0;
+        const int per = (heads + 63) / 64;
+#pragma unroll
+        for (int i = 0; i < BT_MAX_HEADS / 64; ++i) {
+            const int h = tid * per + i;
+            c[i] = (i < per && h < heads) ? count[h] : 0u;
+            s += c[i];
+        }
+        uint32_t before = s;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_up((int)before, d);
+            if (tid >= d) before += o;
+        }
+        before -= s;
+#pragma unroll
+        for (int i = 0; i < BT_MAX_HEADS / 64; ++i) {
+            const int h = tid * per + i;
+            if (i < per && h < heads) {
+                count[h] = base + before;
+                start[h] = base + before;
+                before += c[i];
+                if (h == heads - 1) start[heads] = base + before;
+            }
+        }
+    }
+    __syncthreads();
+    for (uint32_t e = p0 + l; e < p1; e += 8) {
+        const uint32_t ch = bt_entry<BLOCKED>(idx, shift, e), h = ch >> 7;
+        if (h < (uint32_t)heads) {
+            const uint32_t at = atomicAdd(&count[h], 1u);
+            if (at < room) list[at] = (bt_entry<BLOCKED>(val, shift, e) << 16) | ((uint32_t)t << 7) | (ch & 127u);
+        }
+    }
+    __syncthreads();
+}
+
+// Rows of the scaled query: rotated back by the prefix's length for the own tokens (whose positions then start at 0), a power
+// of two to bring the largest to [2^13, 2^14), two parts.  The element order is that of the operand: eight halves for
+// (step t, group g) are the pairs 16 g + 4 t .. + 3.
+__device__ void bt_query_row(const BtArgs &a, const KvqParamsHeader *hdr, int which, int row, int lane)
+{
+    // row: [b][query head]
+    const int b = row / (a.heads * a.ratio), qh = row % (a.heads * a.ratio), h = qh / a.ratio, r = qh % a.ratio;
+    const float f = a.scale * KVQ_LOG2E;
+    float x = a.q[(int64_t)row * 128 + lane] * f, y = a.q[(int64_t)row * 128 + 64 + lane] * f;
+    if (which == 1 && a.prefix > 0) {
+        float c, s;
+        sincospif(2.0f * rope_rev((float)a.prefix, hdr->rope_vh[lane], hdr->rope_vl[lane]), &s, &c);
+        const float x0 = x, y0 = y;
+        x = __builtin_fmaf(x0, c, y0 * s);
+        y = __builtin_fmaf(y0, c, -(x0 * s));
+    }
+    const float m = kvq_wave_max(__builtin_fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)));
+    int e = 0;
+    if (m > 0.0f && m < __builtin_inff()) (void)frexpf(m, &e);
+    x = ldexpf(x, 14 - e);
+    y = ldexpf(y, 14 - e);
+    const int64_t at = which == 0 ? ((int64_t)h * a.n_seqs + b) * a.ratio + r : (int64_t)row;
+    const half2_t hi = {(_Float16)x, (_Float16)y};
+    const half2_t lo = {(_Float16)(x - (float)hi.x), (_Float16)(y - (float)hi.y)};
+    const int g = lane >> 4, t = (lane >> 2) & 3, u = lane & 3;
+    half2_t *o = (half2_t *)(a.w.rows[which] + at * BT_ROW) + (t * 4 + g) * 4 + u;
+    o[0] = hi;
+    o[64] = lo;
+    if (lane == 0) a.w.row_scale[which][at] = ldexpf(1.0f, e - 14);
+}
+
+// First kernel: descriptors from the arguments to memory, outliers by head, query rows.
+__global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, int row_wgs)
+{
+    __shared__ uint32_t count[BT_MAX_HEADS];
+    const int tid = threadIdx.x;
+    int wg = blockIdx.x;
+    if (wg == 0) {
+        const BtSeg *from = s.seg;
+        uint32_t *to = (uint32_t *)(a.w.segs + s.first);
+        const int words = s.n * (int)(sizeof(BtSeg) / 4);
+        for (int i = tid; i < words; i += BT_NT) to[i] = ((const uint32_t *)from)[i];
+    }
+    if (wg < row_wgs) {
+        const int rows = a.n_seqs * a.heads * a.ratio, wave = tid >> 6;
+        const int row = wg * BT_WAVES + wave;
+        if (row >= rows) return;
+        const KvqParamsHeader *hdr = (const KvqParamsHeader *)s.seg[s.n - 1].params;       // the rotary constants are one layer's
+        if (a.prefix > 0) bt_query_row(a, hdr, 0, row, tid & 63);
+        if (a.own) bt_query_row(a, hdr, 1, row, tid & 63);
+        return;
+    }
+    wg -= row_wgs;
+    int i = 0;
+    while (i + 1 < s.n && wg >= s.wg0[i + 1]) ++i;
+    const BtSeg &g = s.seg[i];
+    const int blk = wg - s.wg0[i], n0 = blk * BT_BLOCK;
+    if (n0 >= g.n) return;
+    const int64_t at = (int64_t)(g.blk0 + blk) * (a.heads + 1);
+    if (g.shift == 0) {
+        bt_sort_side<false>(g.k_ptr, g.k_idx, g.k_val, 0, g.k_room, n0, g.n, a.heads, a.w.k_start + at, a.w.k_list + g.k_list, count);
+        bt_sort_side<false>(g.v_ptr, g.v_idx, g.v_val, 0, g.v_room, n0, g.n, a.heads, a.w.v_start + at, a.w.v_list + g.v_list, count);
+    } else {
+        bt_sort_side<true>(g.k_ptr, g.k_idx, g.k_val, g.shift, g.k_room, n0, g.n, a.heads, a.w.k_start + at, a.w.k_list + g.k_list, count);
+        bt_sort_side<true>(g.v_ptr, g.v_idx, g.v_val, g.shift, g.v_room, n0, g.n, a.heads, a.w.v_start + at, a.w.v_list + g.v_list, count);
+    }
+    if (tid < 64) {
+        float m = 0.0f;
+        if (tid < BT_BLOCK && n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
+        m = kvq_wave_max(m);
+        if (tid == 0) a.w.smax[g.blk0 + blk] = m;
+    }
+}
+
+__device__ __forceinline__ void bt_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Maximum over the four lanes of a column.
+__device__ __forceinline__ float bt_column_max(float v)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    v = __builtin_fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    const uint32_t d = __builtin_bit_cast(uint32_t, v);
+    const u32x2 q = __builtin_amdgcn_permlane16_swap(d, d, false, false);
+    return __builtin_fmaxf(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
+
+// (hi, lo) parts of two numbers, packed; `minus_one` is opaque to the compiler, so that hi - x stays one instruction.
+__device__ __forceinline__ void bt_split(float x, float y, float minus_one, uint32_t &hi, uint32_t &lo)
+{
+    const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
+    const half2_t hh = __builtin_bit_cast(half2_t, h);
+    const float a = __builtin_fmaf((float)hh.x, minus_one, x), b = __builtin_fmaf((float)hh.y, minus_one, y);
+    hi = __builtin_bit_cast(uint32_t, h);
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
+
+__device__ __forceinline__ half8_t bt_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_bit_cast(half8_t, uint4{a, b, c, d});
+}
+
+__device__ __forceinline__ float4_t bt_mfma(half8_t a, half8_t b, float4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Second kernel: a workgroup takes `chunk` blocks of one cache for one KV head and 16 MB queries.  WHICH = 0: the prefix,
+// every sequence's queries; 1: a sequence's own tokens, its own queries.
+template <int BITS, int MB, int WHICH>
+__global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArgs a)
+{
+    constexpr int NE = 1 << BITS, FB = 2 * BITS;
+    constexpr uint32_t FMASK = (1u << FB) - 1u;
+    constexpr int QBYTES = 8192 * MB;
+    constexpr int OROW = 132;                              // floats of a query's row of sums (padded)
+    constexpr int SUMS = 16 * MB * OROW * 4, PATCHES = BT_WAVES * BT_PATCH;
+    __shared__ __attribute__((aligned(16))) uint8_t area[SUMS > PATCHES ? SUMS : PATCHES];
+    __shared__ __attribute__((aligned(16))) uint8_t qfrag[QBYTES];
+    __shared__ uint32_t lut_k[NE * NE], lut_v[NE * NE];   // pairs of signposts by field
+    __shared__ __attribute__((aligned(16))) uint32_t con_s[64], con_z[64];          // (channel i, channel i + 64) fp16
+    __shared__ __attribute__((aligned(16))) float con_vh[64];                       // theta_i / 2 pi
+    __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];               // angles at a block's first token
+    __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB], red[BT_WAVES];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, g = lane >> 4;
+    const int n_chunks = a.n_chunks[WHICH], mp = a.mp[WHICH];
+    // grid: query blocks innermost (they read the same codes), then heads, then chunks
+    const int qblocks = mp / (16 * MB);
+    const int qb = blockIdx.x % qblocks, h = (blockIdx.x / qblocks) % a.heads, ch = blockIdx.x / (qblocks * a.heads);
+    int si = 0;
+    if (WHICH == 1) {                                      // the last sequence whose first chunk is not after this one
+        int lo = 1, hi = a.n_seqs + 1;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.w.segs[mid].chunk0 <= ch) lo = mid;
+            else hi = mid;
+        }
+        si = lo;
+    }
+    const BtSeg &sg = a.w.segs[si];
+    const int n = sg.n, n_blocks = (n + BT_BLOCK - 1) / BT_BLOCK;
+    const int b0 = (ch - (WHICH == 1 ? sg.chunk0 : 0)) * a.chunk[WHICH];
+    const int b1 = b0 + a.chunk[WHICH] < n_blocks ? b0 + a.chunk[WHICH] : n_blocks;
+    const int first = sg.n_sink < n ? sg.n_sink : n;       // sink tokens are not attended to here
+    const int n_q = WHICH == 0 ? a.n_seqs * a.ratio : a.ratio;
+    const int64_t row0 = WHICH == 0 ? (int64_t)h * n_q : ((int64_t)(si - 1) * a.heads + h) * n_q;
+
+    // ---- staging
+    {
+        const KvqParamsView pv = kvq_params_view(sg.params, a.heads * KVQ_HEAD_DIM);
+        for (int f = tid; f < NE * NE; f += BT_NT) {
+            const half2_t k = {(_Float16)pv.hdr->lut_k[f & (NE - 1)], (_Float16)pv.hdr->lut_k[f >> BITS]};
+            const half2_t v = {(_Float16)pv.hdr->lut_v[f & (NE - 1)], (_Float16)pv.hdr->lut_v[f >> BITS]};
+            lut_k[f] = __builtin_bit_cast(uint32_t, k);
+            lut_v[f] = __builtin_bit_cast(uint32_t, v);
+        }
+        if (tid < 64) {
+            con_s[tid] = pv.s16[h * 128 + tid] | ((uint32_t)pv.s16[h * 128 + 64 + tid] << 16);
+            con_z[tid] = pv.z16[h * 128 + tid] | ((uint32_t)pv.z16[h * 128 + 64 + tid] << 16);
+            con_vh[tid] = pv.hdr->rope_vh[tid];
+        }
+#pragma unroll
+        for (int i = tid; i < QBYTES / 16; i += BT_NT) {
+            const int l = i & 63, t = (i >> 6) & 3, part = (i >> 8) & 1, mb = i >> 9;
+            const int row = (qb * MB + mb) * 16 + (l & 15);
+            uint4 v = {0u, 0u, 0u, 0u};
+            if (row < n_q) v = *(const uint4 *)(a.w.rows[WHICH] + (row0 + row) * BT_ROW + part * 128 + (t * 4 + (l >> 4)) * 8);
+            *(uint4 *)(qfrag + i * 16) = v;
+        }
+        for (int i = tid; i < PATCHES / 16; i += BT_NT) *(uint4 *)(area + i * 16) = uint4{0u, 0u, 0u, 0u};
+        float m = 0.0f;
+        for (int b = b0 + tid; b < b1; b += BT_NT) m = __builtin_fmaxf(m, a.w.smax[sg.blk0 + b]);
+        m = kvq_wave_max(m);
+        if (lane == 0) red[wave] = m;
+    }
+    const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
+    const float my_vh = hdr->rope_vh[lane], my_vl = hdr->rope_vl[lane];
+    float inv[MB], m_run[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const int row = (qb * MB + mb) * 16 + r16;
+        inv[mb] = row < n_q ? a.w.row_scale[WHICH][row0 + row] : 0.0f;
+        m_run[mb] = KVQ_STAT_FLOOR;
+    }
+    __syncthreads();
+    int kappa;
+    {
+        float m = __builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3]));
+        int e = 0;
+        if (m > 0.0f) (void)frexpf(m, &e);                 // every scale < 2^e
+        kappa = e > 0 ? BT_KAPPA - e : BT_KAPPA;
+    }
+    const float kap = (float)kappa;
+    float minus_one = -1.0f, one = 1.0f;
+    asm("" : "+v"(minus_one), "+v"(one));
+
+    float4_t o[8][MB], lz[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        lz[mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int cb = 0; cb < 8; ++cb) o[cb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    uint8_t *const patch = area + wave * BT_PATCH;
+    const int64_t k_plane = (int64_t)sg.cap * 16 * BITS * h, v_plane = (int64_t)(sg.cap >> 1) * 16 * BITS * 2 * h;
+    const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
+    // this lane's dwords of a Key chunk: BITS of them from dword BITS * g on; of a Value chunk: those with bits 8 BITS r16 on
+    uint32_t k_off[BITS], v_off0, v_off1;
+#pragma unroll
+    for (int i = 0; i < BITS; ++i) k_off[i] = (uint32_t)(((BITS * g + i) >> 2) * 1024 + ((BITS * g + i) & 3) * 4 + r16 * 16);
+    const int v_bit = 4 * FB * r16, v_d0 = v_bit >> 5, v_d1 = (BITS == 3 && v_d0 < 11) ? v_d0 + 1 : v_d0;
+    const uint32_t v_shift = (uint32_t)(v_bit & 31);
+    v_off0 = (uint32_t)((v_d0 >> 2) * 1024 + (v_d0 & 3) * 4 + g * 32);
+    v_off1 = (uint32_t)((v_d1 >> 2) * 1024 + (v_d1 & 3) * 4 + g * 32);
+
+    for (int blk = b0 + wave; blk < b1; blk += BT_WAVES) {
+        const int n0 = blk * BT_BLOCK;
+        // ---- codes, scales, outlier lists
+        const uint8_t *kc = sg.k_codes + k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
+        const uint8_t *vc = sg.v_codes + v_plane + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
+        uint32_t kw[2][BITS];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < BITS; ++i) kw[tb][i] = *(const uint32_t *)(kc + k_off[i] + tb * 256);
+        uint32_t vw[2][2][2];                              // [half][token block][pair]: four fields
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int pr = 0; pr < 2; ++pr) {
+                    const uint8_t *p = vc + hf * v_half + tb * 128 + pr * 16;
+                    uint32_t w = *(const uint32_t *)(p + v_off0);
+                    if (BITS == 3) w = __builtin_amdgcn_alignbit(*(const uint32_t *)(p + v_off1), w, v_shift);
+                    if (BITS == 2) w >>= v_shift;
+                    vw[hf][tb][pr] = w;
+                }
+        uint32_t sz[2][4];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            const uint4 v = *(const uint4 *)(sg.v_sz + n0 + tb * 16 + g * 4);
+            sz[tb][0] = v.x; sz[tb][1] = v.y; sz[tb][2] = v.z; sz[tb][3] = v.w;
+        }
+        const int64_t at = (int64_t)(sg.blk0 + blk) * (a.heads + 1) + h;
+        const uint32_t ks0 = a.w.k_start[at], ks1 = a.w.k_start[at + 1], vs0 = a.w.v_start[at], vs1 = a.w.v_start[at + 1];
+        const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
+        const bool edge = n0 < first || n0 + BT_BLOCK > n;
+
+        // ---- Keys: angles of this lane's pairs at the block's first token; residuals into the patch
+        base[wave][lane] = rope_rev((float)n0, my_vh, my_vl);
+        for (uint32_t e = ks0 + lane; e < ks1; e += 64) {
+            const uint32_t x = k_list[e], t = (x >> 7) & 31u, c = x & 127u, p = c & 63u;
+            const uint32_t place = ((((t >> 4) * 4 + ((p >> 2) & 3)) * 64 + (p >> 4) * 16 + (t & 15)) * 4 + (p & 3)) * 4 + (c >> 6) * 2;
+            *(uint16_t *)(patch + place) = (uint16_t)(x >> 16);
+        }
+        bt_lds_order();
+        float4_t s[2][MB];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) s[tb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint4 sv = *(const uint4 *)&con_s[g * 16 + t * 4], zv = *(const uint4 *)&con_z[g * 16 + t * 4];
+            const float4_t vh = *(const float4_t *)&con_vh[g * 16 + t * 4], ba = *(const float4_t *)&base[wave][g * 16 + t * 4];
+            const uint32_t s4[4] = {sv.x, sv.y, sv.z, sv.w}, z4[4] = {zv.x, zv.y, zv.z, zv.w};
+            half8_t hi[2], lo[2];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const uint4 rv = *(const uint4 *)(patch + ((tb * 4 + t) * 64 + lane) * 16);
+                const uint32_t r4[4] = {rv.x, rv.y, rv.z, rv.w};
+                uint32_t kh[4], kl[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int bit = (4 * t + u) * FB, wi = bit >> 5, sh = bit & 31;
+                    uint32_t f = sh + FB <= 32 ? kw[tb][wi] >> sh : __builtin_amdgcn_alignbit(kw[tb][wi + (sh + FB > 32)], kw[tb][wi], sh);
+                    f &= FMASK;
+                    const half2_t l = __builtin_bit_cast(half2_t, lut_k[f]), sc = __builtin_bit_cast(half2_t, s4[u]),
+                                  zc = __builtin_bit_cast(half2_t, z4[u]), re = __builtin_bit_cast(half2_t, r4[u]);
+                    float ka = __builtin_fmaf((float)l.x, (float)sc.x, (float)zc.x), kb = __builtin_fmaf((float)l.y, (float)sc.y, (float)zc.y);
+                    ka = __builtin_fmaf((float)re.x, one, ka);
+                    kb = __builtin_fmaf((float)re.y, one, kb);
+                    const float rev = __builtin_fmaf((float)(tb * 16 + r16), vh[u], ba[u]);
+                    const float c = __builtin_amdgcn_cosf(rev), sn = __builtin_amdgcn_sinf(rev);
+                    bt_split(__builtin_fmaf(ka, c, -(kb * sn)), __builtin_fmaf(kb, c, ka * sn), minus_one, kh[u], kl[u]);
+                }
+                hi[tb] = bt_half8(kh[0], kh[1], kh[2], kh[3]);
+                lo[tb] = bt_half8(kl[0], kl[1], kl[2], kl[3]);
+            }
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                const half8_t qh = *(const half8_t *)(qfrag + ((mb * 2 * 4 + t) * 64 + lane) * 16);
+                const half8_t ql = *(const half8_t *)(qfrag + (((mb * 2 + 1) * 4 + t) * 64 + lane) * 16);
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
+                    s[tb][mb] = bt_mfma(lo[tb], qh, s[tb][mb]);
+                    s[tb][mb] = bt_mfma(hi[tb], ql, s[tb][mb]);
+                    s[tb][mb] = bt_mfma(hi[tb], qh, s[tb][mb]);
+                }
+            }
+        }
+        // ---- the patch again zero, then the Values' residuals
+        bt_lds_order();
+        for (uint32_t e = ks0 + lane; e < ks1; e += 64) {
+            const uint32_t x = k_list[e], t = (x >> 7) & 31u, c = x & 127u, p = c & 63u;
+            const uint32_t place = ((((t >> 4) * 4 + ((p >> 2) & 3)) * 64 + (p >> 4) * 16 + (t & 15)) * 4 + (p & 3)) * 4 + (c >> 6) * 2;
+            *(uint16_t *)(patch + place) = 0;
+        }
+        bt_lds_order();
+        for (uint32_t e = vs0 + lane; e < vs1; e += 64) {
+            const uint32_t x = v_list[e], t = (x >> 7) & 31u, c = x & 127u, j = c & 63u;
+            const uint32_t place = ((((c >> 6) * 4 + (j & 3)) * 64 + ((t >> 2) & 3) * 16 + (j >> 2)) * 8 + (t >> 4) * 4 + (t & 3)) * 2;
+            *(uint16_t *)(patch + place) = (uint16_t)(x >> 16);
+        }
+        // ---- weights
+        if (edge) {
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = n0 + tb * 16 + g * 4 + i;
+                    const bool in = t >= first && t < n;
+                    if (!in) sz[tb][i] = 0u;
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb)
+                        if (!in) s[tb][mb][i] = -__builtin_inff();
+                }
+        }
+        half8_t ph[MB], pl[MB], wh[MB], wl[MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            float m = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[0][mb][0], s[0][mb][1]), __builtin_fmaxf(s[0][mb][2], s[0][mb][3])),
+                                      __builtin_fmaxf(__builtin_fmaxf(s[1][mb][0], s[1][mb][1]), __builtin_fmaxf(s[1][mb][2], s[1][mb][3])));
+            m = bt_column_max(m) * inv[mb];
+            if (!(m >= KVQ_STAT_FLOOR)) m = KVQ_STAT_FLOOR;      // no token of the block (-inf, or -inf * 0 in a column without a query)
+            if (__ballot(m > m_run[mb] + BT_MAX_SLACK) != 0ull) {
+                const float up = m > m_run[mb] ? m : m_run[mb], f = __builtin_amdgcn_exp2f(m_run[mb] - up);
+                m_run[mb] = up;
+                lz[mb] *= f;
+#pragma unroll
+                for (int cb = 0; cb < 8; ++cb) o[cb][mb] *= f;
+            }
+            const float shift = kap - m_run[mb];
+            uint32_t a_h[4], a_l[4], w_h[4], w_l[4];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i], inv[mb], shift));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i + 1], inv[mb], shift));
+                    const float s0 = (float)__builtin_bit_cast(half2_t, sz[tb][i]).x, s1 = (float)__builtin_bit_cast(half2_t, sz[tb][i + 1]).x;
+                    bt_split(p0, p1, minus_one, a_h[tb * 2 + i / 2], a_l[tb * 2 + i / 2]);
+                    bt_split(p0 * s0, p1 * s1, minus_one, w_h[tb * 2 + i / 2], w_l[tb * 2 + i / 2]);
+                }
+            ph[mb] = bt_half8(a_h[0], a_h[1], a_h[2], a_h[3]);
+            pl[mb] = bt_half8(a_l[0], a_l[1], a_l[2], a_l[3]);
+            wh[mb] = bt_half8(w_h[0], w_h[1], w_h[2], w_h[3]);
+            wl[mb] = bt_half8(w_l[0], w_l[1], w_l[2], w_l[3]);
+        }
+        // ---- sum of p z and sum of p: a channel block of its own with rows (z, 1, 0 ...)
+        {
+            uint32_t x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t z2 = __builtin_amdgcn_perm(sz[i >> 1][(i & 1) * 2 + 1], sz[i >> 1][(i & 1) * 2], 0x07060302u);
+                x[i] = r16 == 0 ? z2 : r16 == 1 ? 0x3C003C00u : 0u;
+            }
+            const half8_t zf = bt_half8(x[0], x[1], x[2], x[3]);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                lz[mb] = bt_mfma(zf, pl[mb], lz[mb]);
+                lz[mb] = bt_mfma(zf, ph[mb], lz[mb]);
+            }
+        }
+        bt_lds_order();
+        // ---- Values
+#pragma unroll
+        for (int cb = 0; cb < 8; ++cb) {
+            constexpr int M4 = (int)FMASK << 2;
+            uint32_t x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = vw[cb >> 2][i >> 1][i & 1];
+                const int sh = FB * (cb & 3) - 2;
+                const uint32_t off = (sh < 0 ? w << -sh : w >> sh) & M4;
+                x[i] = *(const uint32_t *)((const uint8_t *)lut_v + off);
+            }
+            const half8_t vf = bt_half8(x[0], x[1], x[2], x[3]);
+            const half8_t rf = *(const half8_t *)(patch + (cb * 64 + lane) * 16);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                o[cb][mb] = bt_mfma(rf, pl[mb], o[cb][mb]);
+                o[cb][mb] = bt_mfma(vf, wl[mb], o[cb][mb]);
+                o[cb][mb] = bt_mfma(rf, ph[mb], o[cb][mb]);
+                o[cb][mb] = bt_mfma(vf, wh[mb], o[cb][mb]);
+            }
+        }
+        bt_lds_order();
+        for (uint32_t e = vs0 + lane; e < vs1; e += 64) {
+            const uint32_t x = v_list[e], t = (x >> 7) & 31u, c = x & 127u, j = c & 63u;
+            const uint32_t place = ((((c >> 6) * 4 + (j & 3)) * 64 + ((t >> 2) & 3) * 16 + (j >> 2)) * 8 + (t >> 4) * 4 + (t & 3)) * 2;
+            *(uint16_t *)(patch + place) = 0;
+        }
+        bt_lds_order();
+    }
+
+    // ---- the wavefronts' sums to one
+    __syncthreads();
+    if (g == 0)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            wave_m[wave][mb * 16 + r16] = m_run[mb];
+            wave_l[wave][mb * 16 + r16] = lz[mb][1];
+        }
+    __syncthreads();
+    float *sums = (float *)area;
+    float fac[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const int c = mb * 16 + r16;
+        const float m = __builtin_fmaxf(__builtin_fmaxf(wave_m[0][c], wave_m[1][c]), __builtin_fmaxf(wave_m[2][c], wave_m[3][c]));
+        fac[mb] = __builtin_amdgcn_exp2f(m_run[mb] - m - kap);
+    }
+    for (int w = 0; w < BT_WAVES; ++w) {
+        if (wave == w)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                const float z = __shfl(lz[mb][0], r16);
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float4_t *p = (float4_t *)(sums + (mb * 16 + r16) * OROW + hf * 64 + g * 16 + i * 4);
+                        float4_t v = {o[hf * 4 + 0][mb][i] + z, o[hf * 4 + 1][mb][i] + z, o[hf * 4 + 2][mb][i] + z, o[hf * 4 + 3][mb][i] + z};
+                        v *= fac[mb];
+                        *p = w == 0 ? v : *p + v;
+                    }
+            }
+        __syncthreads();
+    }
+    const int64_t slot0 = ((int64_t)ch * a.heads + h) * mp + (int64_t)qb * 16 * MB;
+    for (int i = tid; i < 16 * MB * 32; i += BT_NT) {
+        const int row = i >> 5, c = (i & 31) * 4;
+        if (qb * 16 * MB + row < n_q) *(float4_t *)(a.w.part_o[WHICH] + (slot0 + row) * 128 + c) = *(const float4_t *)(sums + row * OROW + c);
+    }
+    if (tid < 16 * MB && qb * 16 * MB + tid < n_q) {
+        float m = KVQ_STAT_FLOOR, l = 0.0f;
+        for (int w = 0; w < BT_WAVES; ++w) m = __builtin_fmaxf(m, wave_m[w][tid]);
+        for (int w = 0; w < BT_WAVES; ++w) l += wave_l[w][tid] * __builtin_amdgcn_exp2f(wave_m[w][tid] - m - kap);
+        *(float2_t *)(a.w.part_ml[WHICH] + (slot0 + tid) * 2) = float2_t{m, l};
+    }
+    (void)n_chunks;
+}
+
+// Third kernel: a workgroup per (sequence, query head) joins the workgroups' sums and the attention-sink tokens.
+__global__ __launch_bounds__(128) void kvq_batch_join(BtArgs a)
+{
+    __shared__ float part[2], sink_x[2 * KVQ_MAX_SINK];
+    const int tid = threadIdx.x, hq = a.heads * a.ratio, b = blockIdx.x / hq, qh = blockIdx.x % hq;
+    const int h = qh / a.ratio, r = qh % a.ratio;
+    const int64_t q0 = (int64_t)blockIdx.x * 128;
+    float m = KVQ_STAT_FLOOR, l = 0.0f, acc = 0.0f;
+    // sink tokens: scores from their fp16 rows
+    int n_sink[2];
+    for (int k = 0; k < 2; ++k) {
+        const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
+        n_sink[k] = sg.n_sink < sg.n ? sg.n_sink : sg.n;
+        for (int j = 0; j < n_sink[k]; ++j) {
+            float x = 0.0f;
+            if (tid < 64) {
+                const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
+                double rev = (double)(j + (k == 0 ? 0 : a.prefix)) * ((double)hdr->rope_vh[tid] + (double)hdr->rope_vl[tid]);
+                rev -= floor(rev);
+                float c, s;
+                sincospif(2.0f * (float)rev, &s, &c);
+                const uint16_t *row = sg.sink_k + (int64_t)j * a.heads * 128 + h * 128;
+                const float ka = kvq_h2f(row[tid]), kb = kvq_h2f(row[tid + 64]);
+                x = a.q[q0 + tid] * (ka * c - kb * s) + a.q[q0 + 64 + tid] * (kb * c + ka * s);
+                for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+            }
+            if (tid == 0) sink_x[k * KVQ_MAX_SINK + j] = x * a.scale * KVQ_LOG2E;
+        }
+    }
+    if (n_sink[0] + n_sink[1]) __syncthreads();
+    const int c_own = a.own ? a.w.segs[1 + b].chunk0 : 0;
+    const int n_own = a.own ? (a.w.segs[1 + b].n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK) : 0;
+    const int n_pre = a.n_chunks[0];
+    const int64_t at_pre = (int64_t)h * a.mp[0] + b * a.ratio + r, step_pre = (int64_t)a.heads * a.mp[0];
+    const int64_t at_own = ((int64_t)c_own * a.heads + h) * a.mp[1] + r, step_own = (int64_t)a.heads * a.mp[1];
+    for (int i = 0; i < n_pre; ++i) m = __builtin_fmaxf(m, a.w.part_ml[0][(at_pre + i * step_pre) * 2]);
+    for (int i = 0; i < n_own; ++i) m = __builtin_fmaxf(m, a.w.part_ml[1][(at_own + i * step_own) * 2]);
+    for (int k = 0; k < 2; ++k)
+        for (int j = 0; j < n_sink[k]; ++j) m = __builtin_fmaxf(m, sink_x[k * KVQ_MAX_SINK + j]);
+    for (int i = 0; i < n_pre; ++i) {
+        const int64_t s = at_pre + i * step_pre;
+        const float f = __builtin_amdgcn_exp2f(a.w.part_ml[0][s * 2] - m);
+        l = __builtin_fmaf(a.w.part_ml[0][s * 2 + 1], f, l);
+        acc = __builtin_fmaf(a.w.part_o[0][s * 128 + tid], f, acc);
+    }
+    for (int i = 0; i < n_own; ++i) {
+        const int64_t s = at_own + i * step_own;
+        const float f = __builtin_amdgcn_exp2f(a.w.part_ml[1][s * 2] - m);
+        l = __builtin_fmaf(a.w.part_ml[1][s * 2 + 1], f, l);
+        acc = __builtin_fmaf(a.w.part_o[1][s * 128 + tid], f, acc);
+    }
+    for (int k = 0; k < 2; ++k) {
+        const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
+        for (int j = 0; j < n_sink[k]; ++j) {
+            const float f = __builtin_amdgcn_exp2f(sink_x[k * KVQ_MAX_SINK + j] - m);
+            l += f;
+            acc = __builtin_fmaf(kvq_h2f(sg.sink_v[(int64_t)j * a.heads * 128 + h * 128 + tid]), f, acc);
+        }
+    }
+    (void)part;
+    a.out[q0 + tid] = l > 0.0f ? acc / l : 0.0f;
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------
+
+struct BtPlan {
+    BtArgs a;
+    int64_t bytes;
+    int mb[2];
+    int64_t blocks;
+};
+
+int64_t bt_up(int64_t n) { return (n + 255) & ~(int64_t)255; }
+
+int bt_mb(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : 4; }
+
+// The tokens of a call and the places of everything in the workspace (from `base`, which may be null).
+kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs, char *base, BtPlan &p)
+{
+    memset(&p, 0, sizeof p);
+    const kvq_cache *one = prefix;
+    if (n_seqs < 1 || n_seqs > (1 << 20)) return KVQ_ERR_INVALID_ARG;
+    int64_t own_blocks = 0, k_entries = 0, v_entries = 0;
+    auto add = [&](const kvq_cache *c, int64_t &blocks) -> kvq_status {
+        const kvq_status st = kvq_check_cache(c);
+        if (st != KVQ_OK) return st;
+        if (!one) one = c;
+        if (!c->loaded) return KVQ_ERR_NOT_LOADED;
+        if (c->n_tokens_k != c->n_tokens_v) return KVQ_ERR_INVALID_ARG;
+        if (c->bits != one->bits || c->n_kv_heads != one->n_kv_heads || c->n_q_heads != one->n_q_heads || c->rope_base != one->rope_base)
+            return KVQ_ERR_INVALID_ARG;
+        const int64_t n = c->n_tokens_k, most = n * c->n_kv_heads * KVQ_HEAD_DIM;
+        blocks += (n + BT_BLOCK - 1) / BT_BLOCK;
+        k_entries += c->cap_nnz_k < most ? c->cap_nnz_k : most;
+        v_entries += c->cap_nnz_v < most ? c->cap_nnz_v : most;
+        return KVQ_OK;
+    };
+    int64_t pre_blocks = 0;
+    if (prefix) {
+        const kvq_status st = add(prefix, pre_blocks);
+        if (st != KVQ_OK) return st;
+    }
+    for (int32_t b = 0; caches && b < n_seqs; ++b)
+        if (caches[b]) {
+            const kvq_status st = add(caches[b], own_blocks);
+            if (st != KVQ_OK) return st;
+        }
+    if (!one) return KVQ_ERR_INVALID_ARG;
+    BtArgs &a = p.a;
+    a.n_seqs = n_seqs;
+    a.heads = one->n_kv_heads;
+    a.ratio = one->n_q_heads / one->n_kv_heads;
+    a.prefix = prefix ? (int32_t)prefix->n_tokens_k : 0;
+    a.own = own_blocks > 0;
+    p.blocks = pre_blocks + own_blocks;
+    if (p.blocks * (a.heads + 1) >= ((int64_t)1 << 40) || (int64_t)n_seqs * one->n_q_heads >= ((int64_t)1 << 28)) return KVQ_ERR_UNSUPPORTED;
+    const int64_t m[2] = {(int64_t)n_seqs * a.ratio, a.ratio};
+    const int64_t blocks[2] = {pre_blocks, own_blocks};
+    for (int k = 0; k < 2; ++k) {
+        p.mb[k] = bt_mb(m[k]);
+        a.mp[k] = (int32_t)((m[k] + 16 * p.mb[k] - 1) / (16 * p.mb[k]) * (16 * p.mb[k]));
+        // as many workgroups as the chip holds at once (or a little under), none with less than a block per wavefront
+        const int64_t per_head = (int64_t)kvq_cu_count() * (p.mb[k] == 1 ? 3 : 2) / ((int64_t)a.heads * (a.mp[k] / (16 * p.mb[k])));
+        int64_t chunk = per_head > 0 ? (blocks[k] + per_head - 1) / per_head : blocks[k];
+        chunk = (chunk + BT_WAVES - 1) / BT_WAVES * BT_WAVES;
+        if (chunk < BT_WAVES) chunk = BT_WAVES;
+        a.chunk[k] = (int32_t)chunk;
+    }
+    a.n_chunks[0] = (int32_t)((pre_blocks + a.chunk[0] - 1) / a.chunk[0]);
+    int64_t own_chunks = 0;
+    for (int32_t b = 0; caches && b < n_seqs; ++b)
+        if (caches[b]) own_chunks += ((caches[b]->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK + a.chunk[1] - 1) / a.chunk[1];
+    if (own_chunks >= (1 << 24)) return KVQ_ERR_UNSUPPORTED;
+    a.n_chunks[1] = (int32_t)own_chunks;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        char *q = base + at;
+        at += bt_up(bytes);
+        return q;
+    };
+    BtWork &w = a.w;
+    w.segs = (BtSeg *)take((int64_t)sizeof(BtSeg) * (1 + n_seqs));
+    w.k_start = (uint32_t *)take(4 * p.blocks * (a.heads + 1));
+    w.v_start = (uint32_t *)take(4 * p.blocks * (a.heads + 1));
+    w.smax = (float *)take(4 * p.blocks);
+    const int64_t rows = (int64_t)n_seqs * one->n_q_heads;
+    for (int k = 0; k < 2; ++k) {
+        const int64_t here = blocks[k] > 0 ? rows : 0;
+        w.rows[k] = (_Float16 *)take(here * BT_ROW * 2);
+        w.row_scale[k] = (float *)take(here * 4);
+        const int64_t slots = (int64_t)a.n_chunks[k] * a.heads * a.mp[k];
+        w.part_o[k] = (float *)take(slots * 512);
+        w.part_ml[k] = (float *)take(slots * 8);
+    }
+    w.k_list = (uint32_t *)take(4 * k_entries);
+    w.v_list = (uint32_t *)take(4 * v_entries);
+    p.bytes = at > 256 ? at : 256;
+    return KVQ_OK;
+}
+
+template <int BITS, int WHICH>
+kvq_status bt_launch_bits(const BtArgs &a, int mb, hipStream_t s)
+{
+    const int64_t wgs = (int64_t)a.n_chunks[WHICH] * a.heads * (a.mp[WHICH] / (16 * mb));
+    if (wgs == 0) return KVQ_OK;
+    if (wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)wgs), block(BT_NT);
+    if (mb == 1) kvq_batch_attend<BITS, 1, WHICH><<<grid, block, 0, s>>>(a);
+    else if (mb == 2) kvq_batch_attend<BITS, 2, WHICH><<<grid, block, 0, s>>>(a);
+    else kvq_batch_attend<BITS, 4, WHICH><<<grid, block, 0, s>>>(a);
+    KVQ_HIP_CHECK(hipGetLastError());
+    return KVQ_OK;
+}
+
+template <int WHICH>
+kvq_status bt_launch(const BtArgs &a, int bits, int mb, hipStream_t s)
+{
+    if (bits == 2) return bt_launch_bits<2, WHICH>(a, mb, s);
+    if (bits == 3) return bt_launch_bits<3, WHICH>(a, mb, s);
+    return bt_launch_bits<4, WHICH>(a, mb, s);
+}
+
+}  // namespace
+
+extern "C" int64_t kvq_attention_decode_batch_workspace_bytes(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs)
+{
+    BtPlan p;
+    return bt_plan(prefix, caches, n_seqs, nullptr, p) == KVQ_OK ? p.bytes : 0;
+}
+
+extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs,
+                                                 const float *d_q_rot, float scale, float *d_out, void *d_workspace,
+                                                 int64_t workspace_bytes, void *stream)
+{
+    hipStream_t s = (hipStream_t)stream;
+    BtPlan p;
+    kvq_status st = bt_plan(prefix, caches, n_seqs, (char *)d_workspace, p);
+    if (st != KVQ_OK) return st;
+    if (!d_q_rot || !d_out || ((uintptr_t)d_q_rot & 3) || ((uintptr_t)d_out & 3)) return KVQ_ERR_INVALID_ARG;
+    if (!d_workspace || ((uintptr_t)d_workspace & 15)) return KVQ_ERR_INVALID_ARG;
+    if (workspace_bytes < p.bytes) return KVQ_ERR_CAPACITY;
+    BtArgs &a = p.a;
+    a.q = d_q_rot;
+    a.out = d_out;
+    a.scale = scale;
+    const kvq_cache *one = prefix;
+    for (int32_t b = 0; caches && !one && b < n_seqs; ++b) one = caches[b];
+
+    // ---- descriptors, BT_SEGS at a time in the arguments of the first kernel
+    BtSegs part;
+    int64_t k_list = 0, v_list = 0, blk = 0, chunk = 0;
+    int wgs = 0;
+    memset(&part, 0, sizeof part);
+    bool rows_done = false;
+    auto flush = [&]() -> kvq_status {
+        part.wg0[part.n] = wgs;
+        // an empty sequence's descriptor has the constants too (rows read the rotary ones)
+        const int64_t rows = (int64_t)n_seqs * one->n_q_heads;
+        const int row_wgs = rows_done ? 0 : (int)((rows + BT_WAVES - 1) / BT_WAVES);
+        rows_done = true;
+        kvq_batch_prepare<<<dim3((unsigned)(row_wgs + wgs > 0 ? row_wgs + wgs : 1)), dim3(BT_NT), 0, s>>>(a, part, row_wgs);
+        KVQ_HIP_CHECK(hipGetLastError());
+        part.first += part.n;
+        part.n = 0;
+        wgs = 0;
+        return KVQ_OK;
+    };
+    for (int32_t i = 0; i <= n_seqs; ++i) {
+        const kvq_cache *c = i == 0 ? prefix : caches ? caches[i - 1] : nullptr;
+        BtSeg &g = part.seg[part.n];
+        memset(&g, 0, sizeof g);
+        g.params = one->params;
+        g.blk0 = (int32_t)blk;
+        g.chunk0 = (int32_t)chunk;
+        g.k_list = k_list;
+        g.v_list = v_list;
+        part.wg0[part.n] = wgs;
+        if (c && c->n_tokens_k > 0) {
+            g.k_codes = c->k_codes;
+            g.v_codes = c->v_codes;
+            g.v_sz = (const uint32_t *)c->v_sz;
+            g.k_ptr = c->k_ptr;
+            g.v_ptr = c->v_ptr;
+            g.shift = c->nnz_block_shift;
+            g.k_idx = g.shift ? (const void *)c->k_idx_blocks : c->k_idx;
+            g.k_val = g.shift ? (const void *)c->k_val_blocks : c->k_val;
+            g.v_idx = g.shift ? (const void *)c->v_idx_blocks : c->v_idx;
+            g.v_val = g.shift ? (const void *)c->v_val_blocks : c->v_val;
+            g.params = c->params;
+            g.sink_k = c->sink_k;
+            g.sink_v = c->sink_v;
+            g.n = (int32_t)c->n_tokens_k;
+            g.cap = (int32_t)c->cap_tokens;
+            g.n_sink = c->n_sink;
+            const int64_t most = c->n_tokens_k * c->n_kv_heads * KVQ_HEAD_DIM;
+            const int64_t kr = c->cap_nnz_k < most ? c->cap_nnz_k : most, vr = c->cap_nnz_v < most ? c->cap_nnz_v : most;
+            g.k_room = (uint32_t)(kr > 0xFFFFFFFFll ? 0xFFFFFFFFll : kr);
+            g.v_room = (uint32_t)(vr > 0xFFFFFFFFll ? 0xFFFFFFFFll : vr);
+            k_list += kr;
+            v_list += vr;
+            const int64_t nb = (c->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK;
+            blk += nb;
+            wgs += (int)nb;
+            if (i > 0) chunk += (nb + a.chunk[1] - 1) / a.chunk[1];
+        }
+        if (++part.n == BT_SEGS || i == n_seqs) {
+            st = flush();
+            if (st != KVQ_OK) return st;
+        }
+    }
+    st = bt_launch<0>(a, one->bits, p.mb[0], s);
+    if (st == KVQ_OK) st = bt_launch<1>(a, one->bits, p.mb[1], s);
+    if (st != KVQ_OK) return st;
+    kvq_batch_join<<<dim3((unsigned)(n_seqs * one->n_q_heads)), dim3(128), 0, s>>>(a);
+    KVQ_HIP_CHECK(hipGetLastError());
+    return KVQ_OK;
+}
