@@ -92,8 +92,11 @@ __device__ __forceinline__ uint32_t bt_entry(const void *arr, int shift, uint32_
     return ((const uint16_t *const *)arr)[e >> shift][e & ((1u << shift) - 1u)];
 }
 
-// The entries of 32 tokens sorted by head: counted per head, then dealt out.  (Their order within a head is any: every entry
-// has an element of its own.)
+// The entries of 32 tokens sorted by head: eight lanes a token, each entry's rank among its head's from the count it adds to, then
+// its place.  (The order within a head is any: every entry has an element of its own.)  A lane keeps up to BT_HELD entries in
+// registers from the count to the placing; tokens with more (over 48) are read twice instead.
+constexpr int BT_HELD = 6;
+
 template <bool BLOCKED>
 __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int n,
                              int heads, uint32_t *start, uint32_t *list, uint32_t *count)
@@ -107,13 +110,29 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
         p1 = p1 < room ? p1 : room;
     }
     const uint32_t base = ptr[n0];
-    __syncthreads();
-    for (uint32_t e = p0 + l; e < p1; e += 8) {
-        const uint32_t h = bt_entry<BLOCKED>(idx, shift, e) >> 7;
-        if (h < (uint32_t)heads) atomicAdd(&count[h], 1u);
+    uint32_t ch[BT_HELD], x[BT_HELD], rank[BT_HELD];
+#pragma unroll
+    for (int i = 0; i < BT_HELD; ++i) {
+        const uint32_t e = p0 + l + 8 * i;
+        ch[i] = 0xFFFFFFFFu;
+        if (e < p1) {
+            ch[i] = bt_entry<BLOCKED>(idx, shift, e);
+            x[i] = bt_entry<BLOCKED>(val, shift, e);
+        }
+    }
+    const bool many = __syncthreads_or(p1 > p0 && p1 - p0 > 8 * BT_HELD) != 0;
+    if (!many) {
+#pragma unroll
+        for (int i = 0; i < BT_HELD; ++i)
+            if ((ch[i] >> 7) < (uint32_t)heads) rank[i] = atomicAdd(&count[ch[i] >> 7], 1u);
+    } else {
+        for (uint32_t e = p0 + l; e < p1; e += 8) {
+            const uint32_t h = bt_entry<BLOCKED>(idx, shift, e) >> 7;
+            if (h < (uint32_t)heads) atomicAdd(&count[h], 1u);
+        }
     }
     __syncthreads();
-    if (tid < 64) {                                 // exclusive sums, eight heads a lane
+    if (tid < 64) {                                 // exclusive sums, up to eight heads a lane
         uint32_t c[BT_MAX_HEADS / 64], s = 0;
         const int per = (heads + 63) / 64;
 #pragma unroll
@@ -140,14 +159,22 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
         }
     }
     __syncthreads();
-    for (uint32_t e = p0 + l; e < p1; e += 8) {
-        const uint32_t ch = bt_entry<BLOCKED>(idx, shift, e), h = ch >> 7;
-        if (h < (uint32_t)heads) {
-            const uint32_t at = atomicAdd(&count[h], 1u);
-            if (at < room) list[at] = (bt_entry<BLOCKED>(val, shift, e) << 16) | ((uint32_t)t << 7) | (ch & 127u);
+    if (!many) {
+#pragma unroll
+        for (int i = 0; i < BT_HELD; ++i)
+            if ((ch[i] >> 7) < (uint32_t)heads) {
+                const uint32_t at = count[ch[i] >> 7] + rank[i];
+                if (at < room) list[at] = (x[i] << 16) | ((uint32_t)t << 7) | (ch[i] & 127u);
+            }
+    } else {
+        for (uint32_t e = p0 + l; e < p1; e += 8) {
+            const uint32_t c = bt_entry<BLOCKED>(idx, shift, e), h = c >> 7;
+            if (h < (uint32_t)heads) {
+                const uint32_t at = atomicAdd(&count[h], 1u);
+                if (at < room) list[at] = (bt_entry<BLOCKED>(val, shift, e) << 16) | ((uint32_t)t << 7) | (c & 127u);
+            }
         }
     }
-    __syncthreads();
 }
 
 // Rows of the scaled query: rotated back by the prefix's length for the own tokens (whose positions then start at 0), a power
@@ -203,20 +230,21 @@ __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, i
         return;
     }
     wg -= row_wgs;
+    const bool values = wg & 1;                     // a workgroup per side: the chain of each is latency
+    wg >>= 1;
     int i = 0;
     while (i + 1 < s.n && wg >= s.wg0[i + 1]) ++i;
     const BtSeg &g = s.seg[i];
     const int blk = wg - s.wg0[i], n0 = blk * BT_BLOCK;
     if (n0 >= g.n) return;
     const int64_t at = (int64_t)(g.blk0 + blk) * (a.heads + 1);
-    if (g.shift == 0) {
-        bt_sort_side<false>(g.k_ptr, g.k_idx, g.k_val, 0, g.k_room, n0, g.n, a.heads, a.w.k_start + at, a.w.k_list + g.k_list, count);
-        bt_sort_side<false>(g.v_ptr, g.v_idx, g.v_val, 0, g.v_room, n0, g.n, a.heads, a.w.v_start + at, a.w.v_list + g.v_list, count);
-    } else {
-        bt_sort_side<true>(g.k_ptr, g.k_idx, g.k_val, g.shift, g.k_room, n0, g.n, a.heads, a.w.k_start + at, a.w.k_list + g.k_list, count);
-        bt_sort_side<true>(g.v_ptr, g.v_idx, g.v_val, g.shift, g.v_room, n0, g.n, a.heads, a.w.v_start + at, a.w.v_list + g.v_list, count);
-    }
-    if (tid < 64) {
+    const uint32_t *ptr = values ? g.v_ptr : g.k_ptr;
+    const void *idx = values ? g.v_idx : g.k_idx, *val = values ? g.v_val : g.k_val;
+    const uint32_t room = values ? g.v_room : g.k_room;
+    uint32_t *start = (values ? a.w.v_start : a.w.k_start) + at, *list = values ? a.w.v_list + g.v_list : a.w.k_list + g.k_list;
+    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n, a.heads, start, list, count);
+    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n, a.heads, start, list, count);
+    if (values && tid < 64) {
         float m = 0.0f;
         if (tid < BT_BLOCK && n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
         m = kvq_wave_max(m);
@@ -612,21 +640,31 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
     (void)n_chunks;
 }
 
-// Third kernel: a workgroup per (sequence, query head) joins the workgroups' sums and the attention-sink tokens.
-__global__ __launch_bounds__(128) void kvq_batch_join(BtArgs a)
+// Third kernel: a workgroup per (sequence, query head) joins the workgroups' sums and the attention-sink tokens.  Eight slices of
+// 32 threads take every eighth sum, four channels a thread.
+__global__ __launch_bounds__(256) void kvq_batch_join(BtArgs a)
 {
-    __shared__ float part[2], sink_x[2 * KVQ_MAX_SINK];
+    __shared__ float sink_x[2 * KVQ_MAX_SINK], red[4];
+    __shared__ __attribute__((aligned(16))) float sum[8][128], weight[8];
     const int tid = threadIdx.x, hq = a.heads * a.ratio, b = blockIdx.x / hq, qh = blockIdx.x % hq;
-    const int h = qh / a.ratio, r = qh % a.ratio;
+    const int h = qh / a.ratio, r = qh % a.ratio, c4 = (tid & 31) * 4, slice = tid >> 5;
     const int64_t q0 = (int64_t)blockIdx.x * 128;
-    float m = KVQ_STAT_FLOOR, l = 0.0f, acc = 0.0f;
+    const int n_pre = a.n_chunks[0];
+    const int c_own = a.own ? a.w.segs[1 + b].chunk0 : 0;
+    const int n_own = a.own ? (a.w.segs[1 + b].n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK) : 0;
+    const int64_t at_pre = (int64_t)h * a.mp[0] + b * a.ratio + r, step_pre = (int64_t)a.heads * a.mp[0];
+    const int64_t at_own = ((int64_t)c_own * a.heads + h) * a.mp[1] + r, step_own = (int64_t)a.heads * a.mp[1];
+    const int n = n_pre + n_own;
+    auto which = [&](int i) { return i < n_pre ? 0 : 1; };
+    auto slot = [&](int i) { return i < n_pre ? at_pre + i * step_pre : at_own + (int64_t)(i - n_pre) * step_own; };
+    float m = KVQ_STAT_FLOOR;
+    for (int i = tid; i < n; i += 256) m = __builtin_fmaxf(m, a.w.part_ml[which(i)][slot(i) * 2]);
     // sink tokens: scores from their fp16 rows
     int n_sink[2];
     for (int k = 0; k < 2; ++k) {
         const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
         n_sink[k] = sg.n_sink < sg.n ? sg.n_sink : sg.n;
-        for (int j = 0; j < n_sink[k]; ++j) {
-            float x = 0.0f;
+        for (int j = 0; j < n_sink[k]; ++j)
             if (tid < 64) {
                 const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
                 double rev = (double)(j + (k == 0 ? 0 : a.prefix)) * ((double)hdr->rope_vh[tid] + (double)hdr->rope_vl[tid]);
@@ -635,44 +673,48 @@ __global__ __launch_bounds__(128) void kvq_batch_join(BtArgs a)
                 sincospif(2.0f * (float)rev, &s, &c);
                 const uint16_t *row = sg.sink_k + (int64_t)j * a.heads * 128 + h * 128;
                 const float ka = kvq_h2f(row[tid]), kb = kvq_h2f(row[tid + 64]);
-                x = a.q[q0 + tid] * (ka * c - kb * s) + a.q[q0 + 64 + tid] * (kb * c + ka * s);
+                float x = a.q[q0 + tid] * (ka * c - kb * s) + a.q[q0 + 64 + tid] * (kb * c + ka * s);
                 for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+                x *= a.scale * KVQ_LOG2E;
+                if (tid == 0) sink_x[k * KVQ_MAX_SINK + j] = x;
+                m = __builtin_fmaxf(m, x);
             }
-            if (tid == 0) sink_x[k * KVQ_MAX_SINK + j] = x * a.scale * KVQ_LOG2E;
+    }
+    m = kvq_wave_max(m);
+    if ((tid & 63) == 0) red[tid >> 6] = m;
+    __syncthreads();
+    m = __builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3]));
+    float l = 0.0f;
+    float4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = slice; i < n; i += 8) {
+        const int64_t at = slot(i);
+        const float2_t ml = *(const float2_t *)(a.w.part_ml[which(i)] + at * 2);
+        const float f = __builtin_amdgcn_exp2f(ml.x - m);
+        l = __builtin_fmaf(ml.y, f, l);
+        acc += *(const float4_t *)(a.w.part_o[which(i)] + at * 128 + c4) * f;
+    }
+    if (slice == 0)
+        for (int k = 0; k < 2; ++k) {
+            const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
+            for (int j = 0; j < n_sink[k]; ++j) {
+                const float f = __builtin_amdgcn_exp2f(sink_x[k * KVQ_MAX_SINK + j] - m);
+                const uint16_t *row = sg.sink_v + (int64_t)j * a.heads * 128 + h * 128 + c4;
+                l += f;
+                for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(kvq_h2f(row[i]), f, acc[i]);
+            }
         }
-    }
-    if (n_sink[0] + n_sink[1]) __syncthreads();
-    const int c_own = a.own ? a.w.segs[1 + b].chunk0 : 0;
-    const int n_own = a.own ? (a.w.segs[1 + b].n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK) : 0;
-    const int n_pre = a.n_chunks[0];
-    const int64_t at_pre = (int64_t)h * a.mp[0] + b * a.ratio + r, step_pre = (int64_t)a.heads * a.mp[0];
-    const int64_t at_own = ((int64_t)c_own * a.heads + h) * a.mp[1] + r, step_own = (int64_t)a.heads * a.mp[1];
-    for (int i = 0; i < n_pre; ++i) m = __builtin_fmaxf(m, a.w.part_ml[0][(at_pre + i * step_pre) * 2]);
-    for (int i = 0; i < n_own; ++i) m = __builtin_fmaxf(m, a.w.part_ml[1][(at_own + i * step_own) * 2]);
-    for (int k = 0; k < 2; ++k)
-        for (int j = 0; j < n_sink[k]; ++j) m = __builtin_fmaxf(m, sink_x[k * KVQ_MAX_SINK + j]);
-    for (int i = 0; i < n_pre; ++i) {
-        const int64_t s = at_pre + i * step_pre;
-        const float f = __builtin_amdgcn_exp2f(a.w.part_ml[0][s * 2] - m);
-        l = __builtin_fmaf(a.w.part_ml[0][s * 2 + 1], f, l);
-        acc = __builtin_fmaf(a.w.part_o[0][s * 128 + tid], f, acc);
-    }
-    for (int i = 0; i < n_own; ++i) {
-        const int64_t s = at_own + i * step_own;
-        const float f = __builtin_amdgcn_exp2f(a.w.part_ml[1][s * 2] - m);
-        l = __builtin_fmaf(a.w.part_ml[1][s * 2 + 1], f, l);
-        acc = __builtin_fmaf(a.w.part_o[1][s * 128 + tid], f, acc);
-    }
-    for (int k = 0; k < 2; ++k) {
-        const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
-        for (int j = 0; j < n_sink[k]; ++j) {
-            const float f = __builtin_amdgcn_exp2f(sink_x[k * KVQ_MAX_SINK + j] - m);
-            l += f;
-            acc = __builtin_fmaf(kvq_h2f(sg.sink_v[(int64_t)j * a.heads * 128 + h * 128 + tid]), f, acc);
+    *(float4_t *)&sum[slice][c4] = acc;
+    if (c4 == 0) weight[slice] = l;
+    __syncthreads();
+    if (tid < 128) {
+        float o = 0.0f, w = 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            o += sum[i][tid];
+            w += weight[i];
         }
+        a.out[q0 + tid] = w > 0.0f ? o / w : 0.0f;
     }
-    (void)part;
-    a.out[q0 + tid] = l > 0.0f ? acc / l : 0.0f;
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
@@ -832,7 +874,7 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
         const int64_t rows = (int64_t)n_seqs * one->n_q_heads;
         const int row_wgs = rows_done ? 0 : (int)((rows + BT_WAVES - 1) / BT_WAVES);
         rows_done = true;
-        kvq_batch_prepare<<<dim3((unsigned)(row_wgs + wgs > 0 ? row_wgs + wgs : 1)), dim3(BT_NT), 0, s>>>(a, part, row_wgs);
+        kvq_batch_prepare<<<dim3((unsigned)(row_wgs + wgs > 0 ? row_wgs + 2 * wgs : 1)), dim3(BT_NT), 0, s>>>(a, part, row_wgs);
         KVQ_HIP_CHECK(hipGetLastError());
         part.first += part.n;
         part.n = 0;
@@ -885,7 +927,7 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
     st = bt_launch<0>(a, one->bits, p.mb[0], s);
     if (st == KVQ_OK) st = bt_launch<1>(a, one->bits, p.mb[1], s);
     if (st != KVQ_OK) return st;
-    kvq_batch_join<<<dim3((unsigned)(n_seqs * one->n_q_heads)), dim3(128), 0, s>>>(a);
+    kvq_batch_join<<<dim3((unsigned)(n_seqs * one->n_q_heads)), dim3(256), 0, s>>>(a);
     KVQ_HIP_CHECK(hipGetLastError());
     return KVQ_OK;
 }

@@ -6,7 +6,7 @@
 //   Keys    a lane takes a token's chunk of a head: `bits` pieces, each 1 KiB contiguous over a wavefront at both ends.
 //   Values  a lane takes the pair of tokens that share a destination chunk: one chunk if they shared the source's, else two,
 //           their halves of every field put together with a shift of the whole chunk by one code.
-//   outliers, scales and pointers: 16 lanes a token, 256 tokens a workgroup.
+//   outliers, scales and pointers: 256 tokens a workgroup, a run's entries as one contiguous piece.
 // A run's pointers are the source's plus a constant, so a copy is one launch; a list's need the sum of the counts before
 // them, which the first of two launches leaves per 256 tokens.
 #include <string.h>
@@ -51,6 +51,7 @@ struct MvArgs {
 };
 static_assert(sizeof(MvArgs) <= 4000, "kernel arguments");
 
+__host__ __device__ inline int mv_groups(int n) { return (n + MV_GROUP - 1) / MV_GROUP; }
 __host__ __device__ inline int mv_key_items(int at, int n) { return ((at + n + 63) >> 6) - (at >> 6); }
 __host__ __device__ inline int mv_value_items(int at, int n) { return ((at + n + 127) >> 7) - (at >> 7); }
 
@@ -144,6 +145,37 @@ __device__ __forceinline__ void mv_put(void *arr, int shift, uint32_t e, uint16_
     else ((uint16_t *const *)arr)[e >> shift][e & ((1u << shift) - 1u)] = x;
 }
 
+// n consecutive 16-bit entries from place s to place d, by the whole workgroup: where both ends are flat arrays in pieces of 16
+// bytes at the destination's alignment (a source may lie at any even address), four of a thread's under way at a time.
+struct __attribute__((packed, aligned(2))) MvPiece {
+    uint32_t w[4];
+};
+__device__ void mv_entries(const void *src, void *dst, int s_shift, int d_shift, uint32_t s, uint32_t d, uint32_t n)
+{
+    const uint32_t tid = threadIdx.x;
+    if (s_shift | d_shift) {
+        for (uint32_t i = tid; i < n; i += MV_NT) mv_put(dst, d_shift, d + i, mv_get(src, s_shift, s + i));
+        return;
+    }
+    const uint16_t *from = (const uint16_t *)src + s;
+    uint16_t *to = (uint16_t *)dst + d;
+    const uint32_t off = (uint32_t)((8 - (((uintptr_t)to >> 1) & 7)) & 7), head = off < n ? off : n, pieces = (n - head) / 8;
+    if (tid < head) to[tid] = from[tid];
+    from += head;
+    to += head;
+    for (uint32_t i = tid; i < pieces; i += 4 * MV_NT) {
+        MvPiece v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k * MV_NT < pieces) v[k] = *(const MvPiece *)(from + 8 * (size_t)(i + k * MV_NT));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k * MV_NT < pieces) *(uint4 *)(to + 8 * (size_t)(i + k * MV_NT)) = uint4{v[k].w[0], v[k].w[1], v[k].w[2], v[k].w[3]};
+    }
+    const uint32_t done = pieces * 8;
+    if (tid < n - head - done) to[done + tid] = from[done + tid];
+}
+
 // A run's outliers of up to MV_GROUP tokens: pointers are the source's moved by a constant, entries a contiguous piece.
 __device__ void mv_run_side(const MvSide &a, int s_shift, int d_shift, int s0, int d0, int at, int first, int n, int32_t *status)
 {
@@ -154,17 +186,14 @@ __device__ void mv_run_side(const MvSide &a, int s_shift, int d_shift, int s0, i
         const uint64_t e = (uint64_t)base + (s - from);
         return e < a.room ? (uint32_t)e : a.room;
     };
+    const uint32_t p0 = a.s_ptr[s0], e0 = place(p0), e1 = place(a.s_ptr[s0 + n]);
     if (tid < n) {
         const uint32_t s = a.s_ptr[s0 + tid + 1];
         over = (uint64_t)base + (s - from) > a.room;
         a.d_ptr[d0 + tid + 1] = place(s);
     }
-    const uint32_t p0 = a.s_ptr[s0], e0 = place(p0), e1 = place(a.s_ptr[s0 + n]);
-    for (uint32_t e = e0 + tid; e < e1; e += MV_NT) {
-        const uint32_t s = p0 + (e - e0);
-        mv_put(a.d_idx, d_shift, e, mv_get(a.s_idx, s_shift, s));
-        mv_put(a.d_val, d_shift, e, mv_get(a.s_val, s_shift, s));
-    }
+    mv_entries(a.s_idx, a.d_idx, s_shift, d_shift, p0, e0, e1 - e0);
+    mv_entries(a.s_val, a.d_val, s_shift, d_shift, p0, e0, e1 - e0);
     if (over) atomicExch(status, (int32_t)KVQ_ERR_NNZ_OVERFLOW);
 }
 
@@ -199,13 +228,12 @@ __global__ __launch_bounds__(MV_NT) void kvq_move(MvArgs a, const int32_t *__res
     const MvJob &j = a.job[i];
     wg -= a.wg0[i];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int groups = (j.n + MV_GROUP - 1) / MV_GROUP;
+    const int groups = mv_groups(j.n) * (LIST ? 1 : 2);
     if (wg < groups) {
-        const int i0 = wg * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
-        mv_scales<LIST>(j, tokens, a.heads, i0, n);
+        const int i0 = (LIST ? wg : wg >> 1) * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
+        if (LIST || (wg & 1)) mv_scales<LIST>(j, tokens, a.heads, i0, n);
         if (!LIST) {
-            mv_run_side(j.k, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
-            mv_run_side(j.v, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
+            mv_run_side((wg & 1) ? j.v : j.k, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
         } else {
             __shared__ uint32_t part[MV_NT / 64][2];
             const int t = tid < n ? mv_source<true>(j, tokens, i0 + tid) : -1;
@@ -243,48 +271,65 @@ __global__ __launch_bounds__(MV_NT) void kvq_move(MvArgs a, const int32_t *__res
     }
 }
 
-// Second kernel of a gather: pointers and entries of MV_GROUP listed tokens, behind the sums of those before them.
+// Second kernel of a gather: pointers and entries of MV_PART listed tokens, behind the sums of the groups before theirs.  A workgroup
+// counts its whole group; a wavefront copies a token's entries at once, MV_HELD tokens of them under way.
+constexpr int MV_PART = 64, MV_HELD = 4;
 __global__ __launch_bounds__(MV_NT) void kvq_move_lists(MvArgs a, const int32_t *__restrict__ tokens, const uint32_t *__restrict__ sums)
 {
-    __shared__ uint32_t wave_sum[MV_NT / 64], begin[MV_GROUP + 1], from[MV_GROUP];
+    __shared__ uint32_t wave_sum[2][MV_NT / 64], begin[MV_GROUP + 1], from[MV_GROUP];
     const MvJob &j = a.job[0];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wg = blockIdx.x >> 1, side = blockIdx.x & 1;
+    const int side = blockIdx.x & 1, quarter = (blockIdx.x >> 1) & 3, wg = blockIdx.x >> 3;
     const MvSide &s = side == 0 ? j.k : j.v;
     const int i0 = wg * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
+    if (quarter * MV_PART >= n) return;
+    const int t = tid < n ? mv_source<true>(j, tokens, i0 + tid) : -1;
+    const uint32_t p = t < 0 ? 0u : s.s_ptr[t], c = t < 0 ? 0u : s.s_ptr[t + 1] - p;
     uint32_t before = 0;
     for (int i = tid; i < wg; i += MV_NT) before += sums[2 * i + side];
     for (int d = 32; d; d >>= 1) before += (uint32_t)__shfl_xor((int)before, d);
-    if (lane == 0) wave_sum[wave] = before;
-    __syncthreads();
-    const uint64_t base = (uint64_t)s.d_ptr[j.at] + wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
-    __syncthreads();
-    const int t = tid < n ? mv_source<true>(j, tokens, i0 + tid) : -1;
-    const uint32_t p = t < 0 ? 0u : s.s_ptr[t], c = t < 0 ? 0u : s.s_ptr[t + 1] - p;
     uint32_t sum = c;
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t o = (uint32_t)__shfl_up((int)sum, d);
         if (lane >= d) sum += o;
     }
-    if (lane == 63) wave_sum[wave] = sum;
+    if (lane == 63) {
+        wave_sum[0][wave] = before;
+        wave_sum[1][wave] = sum;
+    }
     __syncthreads();
-    for (int w = 0; w < wave; ++w) sum += wave_sum[w];
+    const uint64_t base = (uint64_t)s.d_ptr[j.at] + wave_sum[0][0] + wave_sum[0][1] + wave_sum[0][2] + wave_sum[0][3];
+    for (int w = 0; w < wave; ++w) sum += wave_sum[1][w];
     const uint64_t end = base + sum;
-    const uint32_t clipped = end < s.room ? (uint32_t)end : s.room, started = end - c < s.room ? (uint32_t)(end - c) : s.room;
-    begin[tid] = started;
+    const uint32_t clipped = end < s.room ? (uint32_t)end : s.room;
+    begin[tid] = end - c < s.room ? (uint32_t)(end - c) : s.room;
     from[tid] = p;
     if (tid == MV_GROUP - 1) begin[MV_GROUP] = clipped;
-    if (tid < n) {
+    if (tid < n && wave == quarter) {
         s.d_ptr[j.at + i0 + tid + 1] = clipped;
         if (end > s.room) atomicExch(j.status, (int32_t)KVQ_ERR_NNZ_OVERFLOW);
     }
     __syncthreads();
-    for (int r = tid >> 4; r < n; r += MV_NT / 16) {
-        const uint32_t d0 = begin[r], d1 = begin[r + 1], s0 = from[r];
-        for (uint32_t e = d0 + (tid & 15); e < d1; e += 16) {
-            mv_put(s.d_idx, j.d_shift, e, mv_get(s.s_idx, j.s_shift, s0 + (e - d0)));
-            mv_put(s.d_val, j.d_shift, e, mv_get(s.s_val, j.s_shift, s0 + (e - d0)));
-        }
+    const int last = (quarter + 1) * MV_PART < n ? (quarter + 1) * MV_PART : n;
+    for (int r = quarter * MV_PART + wave * MV_HELD; r < last; r += MV_NT / 64 * MV_HELD) {
+        uint16_t x[MV_HELD], y[MV_HELD];
+#pragma unroll
+        for (int k = 0; k < MV_HELD; ++k)
+            if (r + k < last && begin[r + k] + lane < begin[r + k + 1]) {
+                x[k] = mv_get(s.s_idx, j.s_shift, from[r + k] + lane);
+                y[k] = mv_get(s.s_val, j.s_shift, from[r + k] + lane);
+            }
+#pragma unroll
+        for (int k = 0; k < MV_HELD; ++k)
+            if (r + k < last && begin[r + k] + lane < begin[r + k + 1]) {
+                mv_put(s.d_idx, j.d_shift, begin[r + k] + lane, x[k]);
+                mv_put(s.d_val, j.d_shift, begin[r + k] + lane, y[k]);
+            }
+        for (int k = 0; k < MV_HELD && r + k < last; ++k)          // tokens of more outliers than lanes
+            for (uint32_t e = lane + 64; begin[r + k] + e < begin[r + k + 1]; e += 64) {
+                mv_put(s.d_idx, j.d_shift, begin[r + k] + e, mv_get(s.s_idx, j.s_shift, from[r + k] + e));
+                mv_put(s.d_val, j.d_shift, begin[r + k] + e, mv_get(s.s_val, j.s_shift, from[r + k] + e));
+            }
     }
 }
 
@@ -332,10 +377,10 @@ void mv_job(MvJob &j, const kvq_cache *dst, const kvq_cache *src, int64_t first,
     j.s_sink = src->n_sink; j.d_sink = dst->n_sink;
 }
 
-int64_t mv_wgs(const MvJob &j, int heads, int param_words)
+int64_t mv_wgs(const MvJob &j, int heads, int param_words, bool list)
 {
     const int64_t keys = (int64_t)mv_key_items(j.at, j.n) * heads, values = 2 * (int64_t)mv_value_items(j.at, j.n) * heads;
-    return (j.n + MV_GROUP - 1) / MV_GROUP + (j.s_params ? (param_words + 16 * MV_NT - 1) / (16 * MV_NT) : 0) + (keys + 3) / 4 + (values + 3) / 4;
+    return mv_groups(j.n) * (list ? 1 : 2) + (j.s_params ? (param_words + 16 * MV_NT - 1) / (16 * MV_NT) : 0) + (keys + 3) / 4 + (values + 3) / 4;
 }
 
 template <bool LIST>
@@ -386,7 +431,7 @@ extern "C" kvq_status kvq_cache_copy(kvq_cache *const *dst, const kvq_cache *con
         MvJob &j = a.job[a.n_jobs];
         mv_job(j, dst[i], src[i], first[i], count[i]);
         a.wg0[a.n_jobs++] = (int32_t)wgs;
-        wgs += (count[i] > 0 || j.s_params) ? mv_wgs(j, a.heads, a.param_words) : 0;
+        wgs += (count[i] > 0 || j.s_params) ? mv_wgs(j, a.heads, a.param_words, false) : 0;
         a.wg0[a.n_jobs] = (int32_t)wgs;
         if (a.n_jobs == MV_JOBS || i + 1 == n_copies || wgs > (1 << 28)) {
             if (wgs > 0) {
@@ -417,12 +462,12 @@ extern "C" kvq_status kvq_cache_gather(kvq_cache *dst, const kvq_cache *src, con
     a.n_jobs = 1;
     a.param_words = (int32_t)(kvq_params_bytes(a.heads) / 4);
     mv_job(a.job[0], dst, src, 0, n);
-    const int64_t wgs = mv_wgs(a.job[0], a.heads, a.param_words);
+    const int64_t wgs = mv_wgs(a.job[0], a.heads, a.param_words, true);
     a.wg0[1] = (int32_t)wgs;
     if (wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
     const kvq_status go = mv_launch<true>(a, dst->bits, wgs, d_tokens, (uint32_t *)dst->workspace, (hipStream_t)stream);
     if (go != KVQ_OK) return go;
-    kvq_move_lists<<<dim3((unsigned)(2 * groups)), dim3(MV_NT), 0, (hipStream_t)stream>>>(a, d_tokens, (const uint32_t *)dst->workspace);
+    kvq_move_lists<<<dim3((unsigned)(8 * groups)), dim3(MV_NT), 0, (hipStream_t)stream>>>(a, d_tokens, (const uint32_t *)dst->workspace);
     KVQ_HIP_CHECK(hipGetLastError());
     mv_done(dst, src, n);
     return KVQ_OK;
