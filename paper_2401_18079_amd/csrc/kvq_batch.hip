@@ -290,6 +290,19 @@ __device__ __forceinline__ float4_t bt_mfma(half8_t a, half8_t b, float4_t c)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// Byte of a wavefront's patch for an entry.  Keys: [token block][step t][lane (g, token)][pair u][channel half]; Values:
+// [channel block][lane (g, channel)][token block][token].
+__device__ __forceinline__ uint32_t bt_key_place(uint32_t x)
+{
+    const uint32_t t = (x >> 7) & 31u, c = x & 127u, p = c & 63u;
+    return ((((t >> 4) * 4 + ((p >> 2) & 3)) * 64 + (p >> 4) * 16 + (t & 15)) * 4 + (p & 3)) * 4 + (c >> 6) * 2;
+}
+__device__ __forceinline__ uint32_t bt_value_place(uint32_t x)
+{
+    const uint32_t t = (x >> 7) & 31u, c = x & 127u, j = c & 63u;
+    return ((((c >> 6) * 4 + (j & 3)) * 64 + ((t >> 2) & 3) * 16 + (j >> 2)) * 8 + (t >> 4) * 4 + (t & 3)) * 2;
+}
+
 // Second kernel: a workgroup takes `chunk` blocks of one cache for one KV head and 16 MB queries.  WHICH = 0: the prefix,
 // every sequence's queries; 1: a sequence's own tokens, its own queries.
 template <int BITS, int MB, int WHICH>
@@ -400,17 +413,30 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
     v_off0 = (uint32_t)((v_d0 >> 2) * 1024 + (v_d0 & 3) * 4 + g * 32);
     v_off1 = (uint32_t)((v_d1 >> 2) * 1024 + (v_d1 & 3) * 4 + g * 32);
 
-    for (int blk = b0 + wave; blk < b1; blk += BT_WAVES) {
-        const int n0 = blk * BT_BLOCK;
-        // ---- codes, scales, outlier lists
+    // What a step reads is requested by the step before, as soon as the registers it lands in are free: codes of the Keys after
+    // the scores, scales after the weights, codes of the Values after the output's products, a list's entries (one a lane; lists
+    // of more go on from memory) after the patch has been zeroed.  The lists' places come 64 steps at a time, a step per lane.
+    const int steps = b1 - b0 > wave ? (b1 - b0 - wave + BT_WAVES - 1) / BT_WAVES : 0;
+    const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
+    uint32_t kw[2][BITS], vr[2][2][2], vr1[BITS == 3 ? 2 : 1][2][2], sz[2][4], ke = 0, ve = 0;
+    uint32_t tab_k0 = 0, tab_k1 = 0, tab_v0 = 0, tab_v1 = 0;
+    auto block_of = [&](int step) { return b0 + wave + BT_WAVES * (step < steps ? step : steps - 1); };
+    auto load_table = [&](int step) {
+        const int64_t at = (int64_t)(sg.blk0 + block_of(step + lane)) * (a.heads + 1) + h;
+        tab_k0 = a.w.k_start[at];
+        tab_k1 = a.w.k_start[at + 1];
+        tab_v0 = a.w.v_start[at];
+        tab_v1 = a.w.v_start[at + 1];
+    };
+    auto load_keys = [&](int n0) {
         const uint8_t *kc = sg.k_codes + k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
-        const uint8_t *vc = sg.v_codes + v_plane + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
-        uint32_t kw[2][BITS];
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
             for (int i = 0; i < BITS; ++i) kw[tb][i] = *(const uint32_t *)(kc + k_off[i] + tb * 256);
-        uint32_t vw[2][2][2];                              // [half][token block][pair]: four fields
+    };
+    auto load_values = [&](int n0) {
+        const uint8_t *vc = sg.v_codes + v_plane + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -418,28 +444,46 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
 #pragma unroll
                 for (int pr = 0; pr < 2; ++pr) {
                     const uint8_t *p = vc + hf * v_half + tb * 128 + pr * 16;
-                    uint32_t w = *(const uint32_t *)(p + v_off0);
-                    if (BITS == 3) w = __builtin_amdgcn_alignbit(*(const uint32_t *)(p + v_off1), w, v_shift);
-                    if (BITS == 2) w >>= v_shift;
-                    vw[hf][tb][pr] = w;
+                    vr[hf][tb][pr] = *(const uint32_t *)(p + v_off0);
+                    if (BITS == 3) vr1[hf][tb][pr] = *(const uint32_t *)(p + v_off1);
                 }
-        uint32_t sz[2][4];
+    };
+    auto load_scales = [&](int n0) {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
             const uint4 v = *(const uint4 *)(sg.v_sz + n0 + tb * 16 + g * 4);
             sz[tb][0] = v.x; sz[tb][1] = v.y; sz[tb][2] = v.z; sz[tb][3] = v.w;
         }
-        const int64_t at = (int64_t)(sg.blk0 + blk) * (a.heads + 1) + h;
-        const uint32_t ks0 = a.w.k_start[at], ks1 = a.w.k_start[at + 1], vs0 = a.w.v_start[at], vs1 = a.w.v_start[at + 1];
-        const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
+    };
+    uint32_t ks0 = 0, ks1 = 0, vs0 = 0, vs1 = 0;
+    if (steps > 0) {
+        const int n0 = block_of(0) * BT_BLOCK;
+        load_table(0);
+        load_keys(n0);
+        load_scales(n0);
+        load_values(n0);
+        ks0 = (uint32_t)__builtin_amdgcn_readlane((int)tab_k0, 0);
+        ks1 = (uint32_t)__builtin_amdgcn_readlane((int)tab_k1, 0);
+        vs0 = (uint32_t)__builtin_amdgcn_readlane((int)tab_v0, 0);
+        vs1 = (uint32_t)__builtin_amdgcn_readlane((int)tab_v1, 0);
+        if (ks0 + lane < ks1) ke = k_list[ks0 + lane];
+        if (vs0 + lane < vs1) ve = v_list[vs0 + lane];
+    }
+
+    for (int step = 0; step < steps; ++step) {
+        const int n0 = block_of(step) * BT_BLOCK, next = step + 1, n0_next = block_of(next) * BT_BLOCK;
         const bool edge = n0 < first || n0 + BT_BLOCK > n;
+        if ((next & 63) == 0) load_table(next);
+        const uint32_t ks0_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_k0, next & 63), ks1_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_k1, next & 63);
+        const uint32_t vs0_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_v0, next & 63), vs1_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_v1, next & 63);
 
         // ---- Keys: angles of this lane's pairs at the block's first token; residuals into the patch
         base[wave][lane] = rope_rev((float)n0, my_vh, my_vl);
-        for (uint32_t e = ks0 + lane; e < ks1; e += 64) {
-            const uint32_t x = k_list[e], t = (x >> 7) & 31u, c = x & 127u, p = c & 63u;
-            const uint32_t place = ((((t >> 4) * 4 + ((p >> 2) & 3)) * 64 + (p >> 4) * 16 + (t & 15)) * 4 + (p & 3)) * 4 + (c >> 6) * 2;
-            *(uint16_t *)(patch + place) = (uint16_t)(x >> 16);
+        const uint32_t kp = bt_key_place(ke);
+        if (ks0 + lane < ks1) *(uint16_t *)(patch + kp) = (uint16_t)(ke >> 16);
+        for (uint32_t e = ks0 + 64 + lane; e < ks1; e += 64) {
+            const uint32_t x = k_list[e];
+            *(uint16_t *)(patch + bt_key_place(x)) = (uint16_t)(x >> 16);
         }
         bt_lds_order();
         float4_t s[2][MB];
@@ -487,18 +531,18 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
                 }
             }
         }
+        load_keys(n0_next);
         // ---- the patch again zero, then the Values' residuals
         bt_lds_order();
-        for (uint32_t e = ks0 + lane; e < ks1; e += 64) {
-            const uint32_t x = k_list[e], t = (x >> 7) & 31u, c = x & 127u, p = c & 63u;
-            const uint32_t place = ((((t >> 4) * 4 + ((p >> 2) & 3)) * 64 + (p >> 4) * 16 + (t & 15)) * 4 + (p & 3)) * 4 + (c >> 6) * 2;
-            *(uint16_t *)(patch + place) = 0;
-        }
+        if (ks0 + lane < ks1) *(uint16_t *)(patch + kp) = 0;
+        for (uint32_t e = ks0 + 64 + lane; e < ks1; e += 64) *(uint16_t *)(patch + bt_key_place(k_list[e])) = 0;
+        if (ks0_next + lane < ks1_next) ke = k_list[ks0_next + lane];
         bt_lds_order();
-        for (uint32_t e = vs0 + lane; e < vs1; e += 64) {
-            const uint32_t x = v_list[e], t = (x >> 7) & 31u, c = x & 127u, j = c & 63u;
-            const uint32_t place = ((((c >> 6) * 4 + (j & 3)) * 64 + ((t >> 2) & 3) * 16 + (j >> 2)) * 8 + (t >> 4) * 4 + (t & 3)) * 2;
-            *(uint16_t *)(patch + place) = (uint16_t)(x >> 16);
+        const uint32_t vp = bt_value_place(ve);
+        if (vs0 + lane < vs1) *(uint16_t *)(patch + vp) = (uint16_t)(ve >> 16);
+        for (uint32_t e = vs0 + 64 + lane; e < vs1; e += 64) {
+            const uint32_t x = v_list[e];
+            *(uint16_t *)(patch + bt_value_place(x)) = (uint16_t)(x >> 16);
         }
         // ---- weights
         if (edge) {
@@ -560,6 +604,7 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
                 lz[mb] = bt_mfma(zf, ph[mb], lz[mb]);
             }
         }
+        load_scales(n0_next);
         bt_lds_order();
         // ---- Values
 #pragma unroll
@@ -568,7 +613,9 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
             uint32_t x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t w = vw[cb >> 2][i >> 1][i & 1];
+                uint32_t w = vr[cb >> 2][i >> 1][i & 1];
+                if (BITS == 3) w = __builtin_amdgcn_alignbit(vr1[BITS == 3 ? cb >> 2 : 0][i >> 1][i & 1], w, v_shift);
+                if (BITS == 2) w >>= v_shift;
                 const int sh = FB * (cb & 3) - 2;
                 const uint32_t off = (sh < 0 ? w << -sh : w >> sh) & M4;
                 x[i] = *(const uint32_t *)((const uint8_t *)lut_v + off);
@@ -583,13 +630,13 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
                 o[cb][mb] = bt_mfma(vf, wh[mb], o[cb][mb]);
             }
         }
+        load_values(n0_next);
         bt_lds_order();
-        for (uint32_t e = vs0 + lane; e < vs1; e += 64) {
-            const uint32_t x = v_list[e], t = (x >> 7) & 31u, c = x & 127u, j = c & 63u;
-            const uint32_t place = ((((c >> 6) * 4 + (j & 3)) * 64 + ((t >> 2) & 3) * 16 + (j >> 2)) * 8 + (t >> 4) * 4 + (t & 3)) * 2;
-            *(uint16_t *)(patch + place) = 0;
-        }
+        if (vs0 + lane < vs1) *(uint16_t *)(patch + vp) = 0;
+        for (uint32_t e = vs0 + 64 + lane; e < vs1; e += 64) *(uint16_t *)(patch + bt_value_place(v_list[e])) = 0;
+        if (vs0_next + lane < vs1_next) ve = v_list[vs0_next + lane];
         bt_lds_order();
+        ks0 = ks0_next; ks1 = ks1_next; vs0 = vs0_next; vs1 = vs1_next;
     }
 
     // ---- the wavefronts' sums to one
