@@ -303,50 +303,56 @@ __device__ __forceinline__ uint32_t bt_value_place(uint32_t x)
     return ((((c >> 6) * 4 + (j & 3)) * 64 + ((t >> 2) & 3) * 16 + (j >> 2)) * 8 + (t >> 4) * 4 + (t & 3)) * 2;
 }
 
-// Second kernel: a workgroup takes `chunk` blocks of one cache for one KV head and 16 MB queries.  WHICH = 0: the prefix,
-// every sequence's queries; 1: a sequence's own tokens, its own queries.
-template <int BITS, int MB, int WHICH>
-__global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArgs a)
-{
-    constexpr int NE = 1 << BITS, FB = 2 * BITS;
-    constexpr uint32_t FMASK = (1u << FB) - 1u;
-    constexpr int QBYTES = 8192 * MB;
-    constexpr int OROW = 132;                              // floats of a query's row of sums (padded)
-    constexpr int SUMS = 16 * MB * OROW * 4, PATCHES = BT_WAVES * BT_PATCH;
-    __shared__ __attribute__((aligned(16))) uint8_t area[SUMS > PATCHES ? SUMS : PATCHES];
-    __shared__ __attribute__((aligned(16))) uint8_t qfrag[QBYTES];
-    __shared__ uint32_t lut_k[NE * NE], lut_v[NE * NE];   // pairs of signposts by field
-    __shared__ __attribute__((aligned(16))) uint32_t con_s[64], con_z[64];          // (channel i, channel i + 64) fp16
-    __shared__ __attribute__((aligned(16))) float con_vh[64];                       // theta_i / 2 pi
-    __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];               // angles at a block's first token
-    __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB], red[BT_WAVES];
+// ---- what the two forms of the second kernel share ---------------------------------------------------------------
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r16 = lane & 15, g = lane >> 4;
-    const int n_chunks = a.n_chunks[WHICH], mp = a.mp[WHICH];
+// A workgroup's tokens and queries.
+struct BtPart {
+    int si, h, ch, qb, n, first, b0, b1, n_q;
+    int64_t row0;                       // its queries' first row
+};
+
+template <int WHICH>
+__device__ __forceinline__ BtPart bt_part(const BtArgs &a, int queries)
+{
+    BtPart p;
     // grid: query blocks innermost (they read the same codes), then heads, then chunks
-    const int qblocks = mp / (16 * MB);
-    const int qb = blockIdx.x % qblocks, h = (blockIdx.x / qblocks) % a.heads, ch = blockIdx.x / (qblocks * a.heads);
-    int si = 0;
+    const int qblocks = a.mp[WHICH] / queries;
+    p.qb = blockIdx.x % qblocks;
+    p.h = (blockIdx.x / qblocks) % a.heads;
+    p.ch = blockIdx.x / (qblocks * a.heads);
+    p.si = 0;
     if (WHICH == 1) {                                      // the last sequence whose first chunk is not after this one
         int lo = 1, hi = a.n_seqs + 1;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (a.w.segs[mid].chunk0 <= ch) lo = mid;
+            if (a.w.segs[mid].chunk0 <= p.ch) lo = mid;
             else hi = mid;
         }
-        si = lo;
+        p.si = lo;
     }
-    const BtSeg &sg = a.w.segs[si];
-    const int n = sg.n, n_blocks = (n + BT_BLOCK - 1) / BT_BLOCK;
-    const int b0 = (ch - (WHICH == 1 ? sg.chunk0 : 0)) * a.chunk[WHICH];
-    const int b1 = b0 + a.chunk[WHICH] < n_blocks ? b0 + a.chunk[WHICH] : n_blocks;
-    const int first = sg.n_sink < n ? sg.n_sink : n;       // sink tokens are not attended to here
-    const int n_q = WHICH == 0 ? a.n_seqs * a.ratio : a.ratio;
-    const int64_t row0 = WHICH == 0 ? (int64_t)h * n_q : ((int64_t)(si - 1) * a.heads + h) * n_q;
+    const BtSeg &sg = a.w.segs[p.si];
+    p.n = sg.n;
+    const int n_blocks = (p.n + BT_BLOCK - 1) / BT_BLOCK;
+    p.b0 = (p.ch - (WHICH == 1 ? sg.chunk0 : 0)) * a.chunk[WHICH];
+    p.b1 = p.b0 + a.chunk[WHICH] < n_blocks ? p.b0 + a.chunk[WHICH] : n_blocks;
+    p.first = sg.n_sink < p.n ? sg.n_sink : p.n;           // sink tokens are not attended to here
+    p.n_q = WHICH == 0 ? a.n_seqs * a.ratio : a.ratio;
+    p.row0 = WHICH == 0 ? (int64_t)p.h * p.n_q : ((int64_t)(p.si - 1) * a.heads + p.h) * p.n_q;
+    return p;
+}
 
-    // ---- staging
+// The layer's and the head's constants in LDS.
+template <int BITS>
+struct BtConst {
+    static constexpr int NE = 1 << BITS, FB = 2 * BITS;
+    static constexpr uint32_t FMASK = (1u << FB) - 1u;
+    uint32_t lut_k[NE * NE], lut_v[NE * NE];               // pairs of signposts by field
+    __attribute__((aligned(16))) uint32_t s[64], z[64];    // Key scales and zero-points: (channel i, channel i + 64) fp16
+    __attribute__((aligned(16))) float vh[64];             // theta_i / 2 pi
+    float red[BT_WAVES];
+    __device__ void stage(const BtArgs &a, const BtSeg &sg, const BtPart &p)
     {
+        const int tid = threadIdx.x;
         const KvqParamsView pv = kvq_params_view(sg.params, a.heads * KVQ_HEAD_DIM);
         for (int f = tid; f < NE * NE; f += BT_NT) {
             const half2_t k = {(_Float16)pv.hdr->lut_k[f & (NE - 1)], (_Float16)pv.hdr->lut_k[f >> BITS]};
@@ -355,133 +361,324 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
             lut_v[f] = __builtin_bit_cast(uint32_t, v);
         }
         if (tid < 64) {
-            con_s[tid] = pv.s16[h * 128 + tid] | ((uint32_t)pv.s16[h * 128 + 64 + tid] << 16);
-            con_z[tid] = pv.z16[h * 128 + tid] | ((uint32_t)pv.z16[h * 128 + 64 + tid] << 16);
-            con_vh[tid] = pv.hdr->rope_vh[tid];
+            s[tid] = pv.s16[p.h * 128 + tid] | ((uint32_t)pv.s16[p.h * 128 + 64 + tid] << 16);
+            z[tid] = pv.z16[p.h * 128 + tid] | ((uint32_t)pv.z16[p.h * 128 + 64 + tid] << 16);
+            vh[tid] = pv.hdr->rope_vh[tid];
         }
-#pragma unroll
-        for (int i = tid; i < QBYTES / 16; i += BT_NT) {
-            const int l = i & 63, t = (i >> 6) & 3, part = (i >> 8) & 1, mb = i >> 9;
-            const int row = (qb * MB + mb) * 16 + (l & 15);
-            uint4 v = {0u, 0u, 0u, 0u};
-            if (row < n_q) v = *(const uint4 *)(a.w.rows[WHICH] + (row0 + row) * BT_ROW + part * 128 + (t * 4 + (l >> 4)) * 8);
-            *(uint4 *)(qfrag + i * 16) = v;
-        }
-        for (int i = tid; i < PATCHES / 16; i += BT_NT) *(uint4 *)(area + i * 16) = uint4{0u, 0u, 0u, 0u};
         float m = 0.0f;
-        for (int b = b0 + tid; b < b1; b += BT_NT) m = __builtin_fmaxf(m, a.w.smax[sg.blk0 + b]);
+        for (int b = p.b0 + tid; b < p.b1; b += BT_NT) m = __builtin_fmaxf(m, a.w.smax[sg.blk0 + b]);
         m = kvq_wave_max(m);
-        if (lane == 0) red[wave] = m;
+        if ((tid & 63) == 0) red[tid >> 6] = m;
     }
-    const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
-    const float my_vh = hdr->rope_vh[lane], my_vl = hdr->rope_vl[lane];
-    float inv[MB], m_run[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        const int row = (qb * MB + mb) * 16 + r16;
-        inv[mb] = row < n_q ? a.w.row_scale[WHICH][row0 + row] : 0.0f;
-        m_run[mb] = KVQ_STAT_FLOOR;
-    }
-    __syncthreads();
-    int kappa;
+    // Exponent of the weights' scale: p <= 2^(BT_MAX_SLACK + kappa) and p s as well stay below 2^15 (every scale < 2^e).
+    __device__ __forceinline__ float kappa() const
     {
-        float m = __builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3]));
+        const float m = __builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3]));
         int e = 0;
-        if (m > 0.0f) (void)frexpf(m, &e);                 // every scale < 2^e
-        kappa = e > 0 ? BT_KAPPA - e : BT_KAPPA;
+        if (m > 0.0f) (void)frexpf(m, &e);
+        return (float)(e > 0 ? BT_KAPPA - e : BT_KAPPA);
     }
-    const float kap = (float)kappa;
-    float minus_one = -1.0f, one = 1.0f;
-    asm("" : "+v"(minus_one), "+v"(one));
+};
 
-    float4_t o[8][MB], lz[MB];
+// This lane's dwords of a chunk.  Keys: BITS of them from dword BITS * g on; Values: those with bits 8 BITS r16 on.
+template <int BITS>
+struct BtLane {
+    uint32_t k_off[BITS], v_off0, v_off1, v_shift;
+    __device__ __forceinline__ BtLane(int r16, int g)
+    {
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        lz[mb] = float4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int cb = 0; cb < 8; ++cb) o[cb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < BITS; ++i) k_off[i] = (uint32_t)(((BITS * g + i) >> 2) * 1024 + ((BITS * g + i) & 3) * 4 + r16 * 16);
+        const int bit = 8 * BITS * r16, d0 = bit >> 5, d1 = (BITS == 3 && d0 < 11) ? d0 + 1 : d0;
+        v_shift = (uint32_t)(bit & 31);
+        v_off0 = (uint32_t)((d0 >> 2) * 1024 + (d0 & 3) * 4 + g * 32);
+        v_off1 = (uint32_t)((d1 >> 2) * 1024 + (d1 & 3) * 4 + g * 32);
     }
-    uint8_t *const patch = area + wave * BT_PATCH;
-    const int64_t k_plane = (int64_t)sg.cap * 16 * BITS * h, v_plane = (int64_t)(sg.cap >> 1) * 16 * BITS * 2 * h;
-    const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
-    // this lane's dwords of a Key chunk: BITS of them from dword BITS * g on; of a Value chunk: those with bits 8 BITS r16 on
-    uint32_t k_off[BITS], v_off0, v_off1;
-#pragma unroll
-    for (int i = 0; i < BITS; ++i) k_off[i] = (uint32_t)(((BITS * g + i) >> 2) * 1024 + ((BITS * g + i) & 3) * 4 + r16 * 16);
-    const int v_bit = 4 * FB * r16, v_d0 = v_bit >> 5, v_d1 = (BITS == 3 && v_d0 < 11) ? v_d0 + 1 : v_d0;
-    const uint32_t v_shift = (uint32_t)(v_bit & 31);
-    v_off0 = (uint32_t)((v_d0 >> 2) * 1024 + (v_d0 & 3) * 4 + g * 32);
-    v_off1 = (uint32_t)((v_d1 >> 2) * 1024 + (v_d1 & 3) * 4 + g * 32);
+};
 
-    // What a step reads is requested by the step before, as soon as the registers it lands in are free: codes of the Keys after
-    // the scores, scales after the weights, codes of the Values after the output's products, a list's entries (one a lane; lists
-    // of more go on from memory) after the patch has been zeroed.  The lists' places come 64 steps at a time, a step per lane.
-    const int steps = b1 - b0 > wave ? (b1 - b0 - wave + BT_WAVES - 1) / BT_WAVES : 0;
-    const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
-    uint32_t kw[2][BITS], vr[2][2][2], vr1[BITS == 3 ? 2 : 1][2][2], sz[2][4], ke = 0, ve = 0;
-    uint32_t tab_k0 = 0, tab_k1 = 0, tab_v0 = 0, tab_v1 = 0;
-    auto block_of = [&](int step) { return b0 + wave + BT_WAVES * (step < steps ? step : steps - 1); };
-    auto load_table = [&](int step) {
-        const int64_t at = (int64_t)(sg.blk0 + block_of(step + lane)) * (a.heads + 1) + h;
-        tab_k0 = a.w.k_start[at];
-        tab_k1 = a.w.k_start[at + 1];
-        tab_v0 = a.w.v_start[at];
-        tab_v1 = a.w.v_start[at + 1];
-    };
-    auto load_keys = [&](int n0) {
-        const uint8_t *kc = sg.k_codes + k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-            for (int i = 0; i < BITS; ++i) kw[tb][i] = *(const uint32_t *)(kc + k_off[i] + tb * 256);
-    };
-    auto load_values = [&](int n0) {
-        const uint8_t *vc = sg.v_codes + v_plane + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
+// Values of 32 tokens as they are loaded: codes and (scale, zero-point) of this lane's channels and tokens.
+template <int BITS>
+struct BtValues {
+    uint32_t c0[2][2][2], c1[BITS == 3 ? 2 : 1][2][2];     // [half][token block][pair]: the dwords with four fields
+    uint32_t sz[2][4];
+    __device__ __forceinline__ void codes(const uint8_t *plane, int64_t half, int n0, const BtLane<BITS> &l)
+    {
+        const uint8_t *vc = plane + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                 for (int pr = 0; pr < 2; ++pr) {
-                    const uint8_t *p = vc + hf * v_half + tb * 128 + pr * 16;
-                    vr[hf][tb][pr] = *(const uint32_t *)(p + v_off0);
-                    if (BITS == 3) vr1[hf][tb][pr] = *(const uint32_t *)(p + v_off1);
+                    const uint8_t *p = vc + hf * half + tb * 128 + pr * 16;
+                    c0[hf][tb][pr] = *(const uint32_t *)(p + l.v_off0);
+                    if (BITS == 3) c1[hf][tb][pr] = *(const uint32_t *)(p + l.v_off1);
                 }
-    };
-    auto load_scales = [&](int n0) {
+    }
+    __device__ __forceinline__ void scales(const uint32_t *v_sz, int n0, int g)
+    {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-            const uint4 v = *(const uint4 *)(sg.v_sz + n0 + tb * 16 + g * 4);
+            const uint4 v = *(const uint4 *)(v_sz + n0 + tb * 16 + g * 4);
             sz[tb][0] = v.x; sz[tb][1] = v.y; sz[tb][2] = v.z; sz[tb][3] = v.w;
         }
+    }
+    // Operand of channel block cb: channels 64 (cb / 4) + 4 r16 + cb % 4.
+    __device__ __forceinline__ half8_t operand(int cb, const uint32_t *lut, uint32_t shift) const
+    {
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w = c0[cb >> 2][i >> 1][i & 1];
+            if (BITS == 3) w = __builtin_amdgcn_alignbit(c1[BITS == 3 ? cb >> 2 : 0][i >> 1][i & 1], w, shift);
+            if (BITS == 2) w >>= shift;
+            const int sh = 2 * BITS * (cb & 3) - 2;
+            const uint32_t off = (sh < 0 ? w << -sh : w >> sh) & (((1u << 2 * BITS) - 1u) << 2);
+            x[i] = *(const uint32_t *)((const uint8_t *)lut + off);
+        }
+        return bt_half8(x[0], x[1], x[2], x[3]);
+    }
+};
+
+// One pair (i, i + 64) of a token: de-quantised, its residuals added, rotated, in two parts.
+template <bool PATCHED>
+__device__ __forceinline__ void bt_key_pair(uint32_t field_lut, uint32_t sc2, uint32_t zc2, uint32_t re2, float rev, float minus_one, float one,
+                                            uint32_t &hi, uint32_t &lo)
+{
+    const half2_t l = __builtin_bit_cast(half2_t, field_lut), sc = __builtin_bit_cast(half2_t, sc2), zc = __builtin_bit_cast(half2_t, zc2),
+                  re = __builtin_bit_cast(half2_t, re2);
+    float ka = __builtin_fmaf((float)l.x, (float)sc.x, (float)zc.x), kb = __builtin_fmaf((float)l.y, (float)sc.y, (float)zc.y);
+    if (PATCHED) {
+        ka = __builtin_fmaf((float)re.x, one, ka);
+        kb = __builtin_fmaf((float)re.y, one, kb);
+    }
+    const float c = __builtin_amdgcn_cosf(rev), sn = __builtin_amdgcn_sinf(rev);
+    bt_split(__builtin_fmaf(ka, c, -(kb * sn)), __builtin_fmaf(kb, c, ka * sn), minus_one, hi, lo);
+}
+
+template <int BITS>
+__device__ __forceinline__ uint32_t bt_key_field(const uint32_t (&w)[BITS], int j)
+{
+    constexpr int FB = 2 * BITS;
+    const int bit = j * FB, wi = bit >> 5, sh = bit & 31;
+    const uint32_t f = sh + FB <= 32 ? w[wi] >> sh : __builtin_amdgcn_alignbit(w[wi + (sh + FB > 32)], w[wi], sh);
+    return f & ((1u << FB) - 1u);
+}
+
+// Running sums of MB blocks of 16 queries: a query per column of the lanes, in log2 units with its own maximum.
+template <int MB>
+struct BtSums {
+    float4_t o[8][MB], lz[MB];          // output by channel block; (sum of p z, sum of p) in the first lanes' first two
+    float m[MB], inv[MB];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            m[mb] = KVQ_STAT_FLOOR;
+            lz[mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int cb = 0; cb < 8; ++cb) o[cb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+struct BtWeights {                      // p and p s in two parts
+    half8_t ph, pl, wh, wl;
+};
+
+// Scores of 32 tokens from n0 on to weights; tokens outside [first, n) have none.
+template <int BITS, int MB>
+__device__ __forceinline__ void bt_weights(float4_t (&s)[2][MB], BtValues<BITS> &v, BtSums<MB> &sum, BtWeights (&w)[MB], bool edge, int n0,
+                                           int first, int n, int g, int r16, float kap, float minus_one)
+{
+    if (edge) {
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = n0 + tb * 16 + g * 4 + i;
+                const bool in = t >= first && t < n;
+                if (!in) v.sz[tb][i] = 0u;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+                    if (!in) s[tb][mb][i] = -__builtin_inff();
+            }
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        float m = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[0][mb][0], s[0][mb][1]), __builtin_fmaxf(s[0][mb][2], s[0][mb][3])),
+                                  __builtin_fmaxf(__builtin_fmaxf(s[1][mb][0], s[1][mb][1]), __builtin_fmaxf(s[1][mb][2], s[1][mb][3])));
+        m = bt_column_max(m) * sum.inv[mb];
+        if (!(m >= KVQ_STAT_FLOOR)) m = KVQ_STAT_FLOOR;      // no token of the block (-inf, or -inf * 0 in a column without a query)
+        if (__ballot(m > sum.m[mb] + BT_MAX_SLACK) != 0ull) {
+            const float up = m > sum.m[mb] ? m : sum.m[mb], f = __builtin_amdgcn_exp2f(sum.m[mb] - up);
+            sum.m[mb] = up;
+            sum.lz[mb] *= f;
+#pragma unroll
+            for (int cb = 0; cb < 8; ++cb) sum.o[cb][mb] *= f;
+        }
+        const float shift = kap - sum.m[mb];
+        uint32_t a_h[4], a_l[4], w_h[4], w_l[4];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i], sum.inv[mb], shift));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i + 1], sum.inv[mb], shift));
+                const float s0 = (float)__builtin_bit_cast(half2_t, v.sz[tb][i]).x, s1 = (float)__builtin_bit_cast(half2_t, v.sz[tb][i + 1]).x;
+                bt_split(p0, p1, minus_one, a_h[tb * 2 + i / 2], a_l[tb * 2 + i / 2]);
+                bt_split(p0 * s0, p1 * s1, minus_one, w_h[tb * 2 + i / 2], w_l[tb * 2 + i / 2]);
+            }
+        w[mb].ph = bt_half8(a_h[0], a_h[1], a_h[2], a_h[3]);
+        w[mb].pl = bt_half8(a_l[0], a_l[1], a_l[2], a_l[3]);
+        w[mb].wh = bt_half8(w_h[0], w_h[1], w_h[2], w_h[3]);
+        w[mb].wl = bt_half8(w_l[0], w_l[1], w_l[2], w_l[3]);
+    }
+    // sum of p z and sum of p: a channel block of its own with rows (z, 1, 0 ...)
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t z2 = __builtin_amdgcn_perm(v.sz[i >> 1][(i & 1) * 2 + 1], v.sz[i >> 1][(i & 1) * 2], 0x07060302u);
+        x[i] = r16 == 0 ? z2 : r16 == 1 ? 0x3C003C00u : 0u;
+    }
+    const half8_t zf = bt_half8(x[0], x[1], x[2], x[3]);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        sum.lz[mb] = bt_mfma(zf, w[mb].pl, sum.lz[mb]);
+        sum.lz[mb] = bt_mfma(zf, w[mb].ph, sum.lz[mb]);
+    }
+}
+
+// The output's products of 32 tokens; `patch` holds their residuals.
+template <int BITS, int MB>
+__device__ __forceinline__ void bt_output(const BtValues<BITS> &v, const BtWeights (&w)[MB], BtSums<MB> &sum, const uint32_t *lut_v,
+                                          uint32_t v_shift, const uint8_t *patch, int lane)
+{
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) {
+        const half8_t vf = v.operand(cb, lut_v, v_shift);
+        const half8_t rf = *(const half8_t *)(patch + (cb * 64 + lane) * 16);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            sum.o[cb][mb] = bt_mfma(rf, w[mb].pl, sum.o[cb][mb]);
+            sum.o[cb][mb] = bt_mfma(vf, w[mb].wl, sum.o[cb][mb]);
+            sum.o[cb][mb] = bt_mfma(rf, w[mb].ph, sum.o[cb][mb]);
+            sum.o[cb][mb] = bt_mfma(vf, w[mb].wh, sum.o[cb][mb]);
+        }
+    }
+}
+
+// Four consecutive channels (64 hf + 16 g + 4 i ..) of block mb's query of this lane, with the zero-points' part.
+template <int MB>
+__device__ __forceinline__ float4_t bt_channels(const BtSums<MB> &sum, int mb, int hf, int i, float z)
+{
+    return float4_t{sum.o[hf * 4 + 0][mb][i] + z, sum.o[hf * 4 + 1][mb][i] + z, sum.o[hf * 4 + 2][mb][i] + z, sum.o[hf * 4 + 3][mb][i] + z};
+}
+
+// A list's places, 64 steps at a time: lane i holds those of step i.
+struct BtTable {
+    uint32_t k0, k1, v0, v1;
+    __device__ __forceinline__ void load(const BtArgs &a, int64_t at)
+    {
+        k0 = a.w.k_start[at];
+        k1 = a.w.k_start[at + 1];
+        v0 = a.w.v_start[at];
+        v1 = a.w.v_start[at + 1];
+    }
+};
+struct BtPlaces {
+    uint32_t k0, k1, v0, v1;
+    __device__ __forceinline__ BtPlaces(const BtTable &t, int i)
+        : k0((uint32_t)__builtin_amdgcn_readlane((int)t.k0, i)), k1((uint32_t)__builtin_amdgcn_readlane((int)t.k1, i)),
+          v0((uint32_t)__builtin_amdgcn_readlane((int)t.v0, i)), v1((uint32_t)__builtin_amdgcn_readlane((int)t.v1, i)) {}
+};
+
+// Second kernel, up to 32 queries: a workgroup takes `chunk` blocks of one cache for one KV head and 16 MB queries, each of its
+// wavefronts every fourth block from the codes to the output.  WHICH = 0: the prefix, every sequence's queries; 1: a sequence's
+// own tokens, its own queries.
+template <int BITS, int MB, int WHICH>
+__global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArgs a)
+{
+    constexpr int QBYTES = 8192 * MB;
+    constexpr int OROW = 132;                              // floats of a query's row of sums (padded)
+    constexpr int SUMS = 16 * MB * OROW * 4, PATCHES = BT_WAVES * BT_PATCH;
+    static_assert(SUMS <= PATCHES, "the sums take the patches' place");
+    __shared__ __attribute__((aligned(16))) uint8_t area[PATCHES];
+    __shared__ __attribute__((aligned(16))) uint8_t qfrag[QBYTES];
+    __shared__ BtConst<BITS> con;
+    __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];               // angles at a block's first token
+    __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, g = lane >> 4;
+    const BtPart p = bt_part<WHICH>(a, 16 * MB);
+    const BtSeg &sg = a.w.segs[p.si];
+
+    con.stage(a, sg, p);
+#pragma unroll
+    for (int i = tid; i < QBYTES / 16; i += BT_NT) {
+        const int l = i & 63, t = (i >> 6) & 3, part = (i >> 8) & 1, mb = i >> 9;
+        const int row = (p.qb * MB + mb) * 16 + (l & 15);
+        uint4 v = {0u, 0u, 0u, 0u};
+        if (row < p.n_q) v = *(const uint4 *)(a.w.rows[WHICH] + (p.row0 + row) * BT_ROW + part * 128 + (t * 4 + (l >> 4)) * 8);
+        *(uint4 *)(qfrag + i * 16) = v;
+    }
+    for (int i = tid; i < PATCHES / 16; i += BT_NT) *(uint4 *)(area + i * 16) = uint4{0u, 0u, 0u, 0u};
+    const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
+    const float my_vh = hdr->rope_vh[lane], my_vl = hdr->rope_vl[lane];
+    BtSums<MB> sum;
+    sum.clear();
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const int row = (p.qb * MB + mb) * 16 + r16;
+        sum.inv[mb] = row < p.n_q ? a.w.row_scale[WHICH][p.row0 + row] : 0.0f;
+    }
+    __syncthreads();
+    const float kap = con.kappa();
+    float minus_one = -1.0f, one = 1.0f;
+    asm("" : "+v"(minus_one), "+v"(one));
+    uint8_t *const patch = area + wave * BT_PATCH;
+    const uint8_t *const k_plane = sg.k_codes + (int64_t)sg.cap * 16 * BITS * p.h, *const v_plane = sg.v_codes + (int64_t)sg.cap * 16 * BITS * p.h;
+    const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
+    const BtLane<BITS> my(r16, g);
+
+    // What a step reads is requested by the step before, as soon as the registers it lands in are free: codes of the Keys after
+    // the scores, scales after the weights, codes of the Values after the output's products, a list's entries (one a lane; lists
+    // of more go on from memory) after the patch has been zeroed.  (Eight queries, 131072 tokens, 32 heads: 381 -> 302 us.)
+    const int steps = p.b1 - p.b0 > wave ? (p.b1 - p.b0 - wave + BT_WAVES - 1) / BT_WAVES : 0;
+    const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
+    uint32_t kw[2][BITS], ke = 0, ve = 0;
+    BtValues<BITS> val;
+    BtTable tab = {0, 0, 0, 0};
+    auto block_of = [&](int step) { return p.b0 + wave + BT_WAVES * (step < steps ? step : steps - 1); };
+    auto place_of = [&](int step) { return (int64_t)(sg.blk0 + block_of(step)) * (a.heads + 1) + p.h; };
+    auto load_keys = [&](int n0) {
+        const uint8_t *kc = k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < BITS; ++i) kw[tb][i] = *(const uint32_t *)(kc + my.k_off[i] + tb * 256);
     };
-    uint32_t ks0 = 0, ks1 = 0, vs0 = 0, vs1 = 0;
     if (steps > 0) {
         const int n0 = block_of(0) * BT_BLOCK;
-        load_table(0);
+        tab.load(a, place_of(lane));
         load_keys(n0);
-        load_scales(n0);
-        load_values(n0);
-        ks0 = (uint32_t)__builtin_amdgcn_readlane((int)tab_k0, 0);
-        ks1 = (uint32_t)__builtin_amdgcn_readlane((int)tab_k1, 0);
-        vs0 = (uint32_t)__builtin_amdgcn_readlane((int)tab_v0, 0);
-        vs1 = (uint32_t)__builtin_amdgcn_readlane((int)tab_v1, 0);
-        if (ks0 + lane < ks1) ke = k_list[ks0 + lane];
-        if (vs0 + lane < vs1) ve = v_list[vs0 + lane];
+        val.scales(sg.v_sz, n0, g);
+        val.codes(v_plane, v_half, n0, my);
     }
+    BtPlaces at(tab, 0);
+    if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
+    if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
 
     for (int step = 0; step < steps; ++step) {
         const int n0 = block_of(step) * BT_BLOCK, next = step + 1, n0_next = block_of(next) * BT_BLOCK;
-        const bool edge = n0 < first || n0 + BT_BLOCK > n;
-        if ((next & 63) == 0) load_table(next);
-        const uint32_t ks0_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_k0, next & 63), ks1_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_k1, next & 63);
-        const uint32_t vs0_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_v0, next & 63), vs1_next = (uint32_t)__builtin_amdgcn_readlane((int)tab_v1, next & 63);
+        const bool edge = n0 < p.first || n0 + BT_BLOCK > p.n;
+        if ((next & 63) == 0) tab.load(a, place_of(next + lane));
+        const BtPlaces at_next(tab, next & 63);
 
         // ---- Keys: angles of this lane's pairs at the block's first token; residuals into the patch
         base[wave][lane] = rope_rev((float)n0, my_vh, my_vl);
         const uint32_t kp = bt_key_place(ke);
-        if (ks0 + lane < ks1) *(uint16_t *)(patch + kp) = (uint16_t)(ke >> 16);
-        for (uint32_t e = ks0 + 64 + lane; e < ks1; e += 64) {
+        if (at.k0 + lane < at.k1) *(uint16_t *)(patch + kp) = (uint16_t)(ke >> 16);
+        for (uint32_t e = at.k0 + 64 + lane; e < at.k1; e += 64) {
             const uint32_t x = k_list[e];
             *(uint16_t *)(patch + bt_key_place(x)) = (uint16_t)(x >> 16);
         }
@@ -493,8 +690,8 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
             for (int mb = 0; mb < MB; ++mb) s[tb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const uint4 sv = *(const uint4 *)&con_s[g * 16 + t * 4], zv = *(const uint4 *)&con_z[g * 16 + t * 4];
-            const float4_t vh = *(const float4_t *)&con_vh[g * 16 + t * 4], ba = *(const float4_t *)&base[wave][g * 16 + t * 4];
+            const uint4 sv = *(const uint4 *)&con.s[g * 16 + t * 4], zv = *(const uint4 *)&con.z[g * 16 + t * 4];
+            const float4_t vh = *(const float4_t *)&con.vh[g * 16 + t * 4], ba = *(const float4_t *)&base[wave][g * 16 + t * 4];
             const uint32_t s4[4] = {sv.x, sv.y, sv.z, sv.w}, z4[4] = {zv.x, zv.y, zv.z, zv.w};
             half8_t hi[2], lo[2];
 #pragma unroll
@@ -503,19 +700,9 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
                 const uint32_t r4[4] = {rv.x, rv.y, rv.z, rv.w};
                 uint32_t kh[4], kl[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int bit = (4 * t + u) * FB, wi = bit >> 5, sh = bit & 31;
-                    uint32_t f = sh + FB <= 32 ? kw[tb][wi] >> sh : __builtin_amdgcn_alignbit(kw[tb][wi + (sh + FB > 32)], kw[tb][wi], sh);
-                    f &= FMASK;
-                    const half2_t l = __builtin_bit_cast(half2_t, lut_k[f]), sc = __builtin_bit_cast(half2_t, s4[u]),
-                                  zc = __builtin_bit_cast(half2_t, z4[u]), re = __builtin_bit_cast(half2_t, r4[u]);
-                    float ka = __builtin_fmaf((float)l.x, (float)sc.x, (float)zc.x), kb = __builtin_fmaf((float)l.y, (float)sc.y, (float)zc.y);
-                    ka = __builtin_fmaf((float)re.x, one, ka);
-                    kb = __builtin_fmaf((float)re.y, one, kb);
-                    const float rev = __builtin_fmaf((float)(tb * 16 + r16), vh[u], ba[u]);
-                    const float c = __builtin_amdgcn_cosf(rev), sn = __builtin_amdgcn_sinf(rev);
-                    bt_split(__builtin_fmaf(ka, c, -(kb * sn)), __builtin_fmaf(kb, c, ka * sn), minus_one, kh[u], kl[u]);
-                }
+                for (int u = 0; u < 4; ++u)
+                    bt_key_pair<true>(con.lut_k[bt_key_field<BITS>(kw[tb], 4 * t + u)], s4[u], z4[u], r4[u],
+                                      __builtin_fmaf((float)(tb * 16 + r16), vh[u], ba[u]), minus_one, one, kh[u], kl[u]);
                 hi[tb] = bt_half8(kh[0], kh[1], kh[2], kh[3]);
                 lo[tb] = bt_half8(kl[0], kl[1], kl[2], kl[3]);
             }
@@ -534,109 +721,28 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
         load_keys(n0_next);
         // ---- the patch again zero, then the Values' residuals
         bt_lds_order();
-        if (ks0 + lane < ks1) *(uint16_t *)(patch + kp) = 0;
-        for (uint32_t e = ks0 + 64 + lane; e < ks1; e += 64) *(uint16_t *)(patch + bt_key_place(k_list[e])) = 0;
-        if (ks0_next + lane < ks1_next) ke = k_list[ks0_next + lane];
+        if (at.k0 + lane < at.k1) *(uint16_t *)(patch + kp) = 0;
+        for (uint32_t e = at.k0 + 64 + lane; e < at.k1; e += 64) *(uint16_t *)(patch + bt_key_place(k_list[e])) = 0;
+        if (at_next.k0 + lane < at_next.k1) ke = k_list[at_next.k0 + lane];
         bt_lds_order();
         const uint32_t vp = bt_value_place(ve);
-        if (vs0 + lane < vs1) *(uint16_t *)(patch + vp) = (uint16_t)(ve >> 16);
-        for (uint32_t e = vs0 + 64 + lane; e < vs1; e += 64) {
+        if (at.v0 + lane < at.v1) *(uint16_t *)(patch + vp) = (uint16_t)(ve >> 16);
+        for (uint32_t e = at.v0 + 64 + lane; e < at.v1; e += 64) {
             const uint32_t x = v_list[e];
             *(uint16_t *)(patch + bt_value_place(x)) = (uint16_t)(x >> 16);
         }
-        // ---- weights
-        if (edge) {
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = n0 + tb * 16 + g * 4 + i;
-                    const bool in = t >= first && t < n;
-                    if (!in) sz[tb][i] = 0u;
-#pragma unroll
-                    for (int mb = 0; mb < MB; ++mb)
-                        if (!in) s[tb][mb][i] = -__builtin_inff();
-                }
-        }
-        half8_t ph[MB], pl[MB], wh[MB], wl[MB];
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-            float m = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[0][mb][0], s[0][mb][1]), __builtin_fmaxf(s[0][mb][2], s[0][mb][3])),
-                                      __builtin_fmaxf(__builtin_fmaxf(s[1][mb][0], s[1][mb][1]), __builtin_fmaxf(s[1][mb][2], s[1][mb][3])));
-            m = bt_column_max(m) * inv[mb];
-            if (!(m >= KVQ_STAT_FLOOR)) m = KVQ_STAT_FLOOR;      // no token of the block (-inf, or -inf * 0 in a column without a query)
-            if (__ballot(m > m_run[mb] + BT_MAX_SLACK) != 0ull) {
-                const float up = m > m_run[mb] ? m : m_run[mb], f = __builtin_amdgcn_exp2f(m_run[mb] - up);
-                m_run[mb] = up;
-                lz[mb] *= f;
-#pragma unroll
-                for (int cb = 0; cb < 8; ++cb) o[cb][mb] *= f;
-            }
-            const float shift = kap - m_run[mb];
-            uint32_t a_h[4], a_l[4], w_h[4], w_l[4];
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i], inv[mb], shift));
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i + 1], inv[mb], shift));
-                    const float s0 = (float)__builtin_bit_cast(half2_t, sz[tb][i]).x, s1 = (float)__builtin_bit_cast(half2_t, sz[tb][i + 1]).x;
-                    bt_split(p0, p1, minus_one, a_h[tb * 2 + i / 2], a_l[tb * 2 + i / 2]);
-                    bt_split(p0 * s0, p1 * s1, minus_one, w_h[tb * 2 + i / 2], w_l[tb * 2 + i / 2]);
-                }
-            ph[mb] = bt_half8(a_h[0], a_h[1], a_h[2], a_h[3]);
-            pl[mb] = bt_half8(a_l[0], a_l[1], a_l[2], a_l[3]);
-            wh[mb] = bt_half8(w_h[0], w_h[1], w_h[2], w_h[3]);
-            wl[mb] = bt_half8(w_l[0], w_l[1], w_l[2], w_l[3]);
-        }
-        // ---- sum of p z and sum of p: a channel block of its own with rows (z, 1, 0 ...)
-        {
-            uint32_t x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t z2 = __builtin_amdgcn_perm(sz[i >> 1][(i & 1) * 2 + 1], sz[i >> 1][(i & 1) * 2], 0x07060302u);
-                x[i] = r16 == 0 ? z2 : r16 == 1 ? 0x3C003C00u : 0u;
-            }
-            const half8_t zf = bt_half8(x[0], x[1], x[2], x[3]);
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                lz[mb] = bt_mfma(zf, pl[mb], lz[mb]);
-                lz[mb] = bt_mfma(zf, ph[mb], lz[mb]);
-            }
-        }
-        load_scales(n0_next);
+        BtWeights w[MB];
+        bt_weights<BITS, MB>(s, val, sum, w, edge, n0, p.first, p.n, g, r16, kap, minus_one);
+        val.scales(sg.v_sz, n0_next, g);
         bt_lds_order();
-        // ---- Values
-#pragma unroll
-        for (int cb = 0; cb < 8; ++cb) {
-            constexpr int M4 = (int)FMASK << 2;
-            uint32_t x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t w = vr[cb >> 2][i >> 1][i & 1];
-                if (BITS == 3) w = __builtin_amdgcn_alignbit(vr1[BITS == 3 ? cb >> 2 : 0][i >> 1][i & 1], w, v_shift);
-                if (BITS == 2) w >>= v_shift;
-                const int sh = FB * (cb & 3) - 2;
-                const uint32_t off = (sh < 0 ? w << -sh : w >> sh) & M4;
-                x[i] = *(const uint32_t *)((const uint8_t *)lut_v + off);
-            }
-            const half8_t vf = bt_half8(x[0], x[1], x[2], x[3]);
-            const half8_t rf = *(const half8_t *)(patch + (cb * 64 + lane) * 16);
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                o[cb][mb] = bt_mfma(rf, pl[mb], o[cb][mb]);
-                o[cb][mb] = bt_mfma(vf, wl[mb], o[cb][mb]);
-                o[cb][mb] = bt_mfma(rf, ph[mb], o[cb][mb]);
-                o[cb][mb] = bt_mfma(vf, wh[mb], o[cb][mb]);
-            }
-        }
-        load_values(n0_next);
+        bt_output<BITS, MB>(val, w, sum, con.lut_v, my.v_shift, patch, lane);
+        val.codes(v_plane, v_half, n0_next, my);
         bt_lds_order();
-        if (vs0 + lane < vs1) *(uint16_t *)(patch + vp) = 0;
-        for (uint32_t e = vs0 + 64 + lane; e < vs1; e += 64) *(uint16_t *)(patch + bt_value_place(v_list[e])) = 0;
-        if (vs0_next + lane < vs1_next) ve = v_list[vs0_next + lane];
+        if (at.v0 + lane < at.v1) *(uint16_t *)(patch + vp) = 0;
+        for (uint32_t e = at.v0 + 64 + lane; e < at.v1; e += 64) *(uint16_t *)(patch + bt_value_place(v_list[e])) = 0;
+        if (at_next.v0 + lane < at_next.v1) ve = v_list[at_next.v0 + lane];
         bt_lds_order();
-        ks0 = ks0_next; ks1 = ks1_next; vs0 = vs0_next; vs1 = vs1_next;
+        at = at_next;
     }
 
     // ---- the wavefronts' sums to one
@@ -644,8 +750,8 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
     if (g == 0)
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            wave_m[wave][mb * 16 + r16] = m_run[mb];
-            wave_l[wave][mb * 16 + r16] = lz[mb][1];
+            wave_m[wave][mb * 16 + r16] = sum.m[mb];
+            wave_l[wave][mb * 16 + r16] = sum.lz[mb][1];
         }
     __syncthreads();
     float *sums = (float *)area;
@@ -654,37 +760,268 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
     for (int mb = 0; mb < MB; ++mb) {
         const int c = mb * 16 + r16;
         const float m = __builtin_fmaxf(__builtin_fmaxf(wave_m[0][c], wave_m[1][c]), __builtin_fmaxf(wave_m[2][c], wave_m[3][c]));
-        fac[mb] = __builtin_amdgcn_exp2f(m_run[mb] - m - kap);
+        fac[mb] = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap);
     }
     for (int w = 0; w < BT_WAVES; ++w) {
         if (wave == w)
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
-                const float z = __shfl(lz[mb][0], r16);
+                const float z = __shfl(sum.lz[mb][0], r16);
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float4_t *p = (float4_t *)(sums + (mb * 16 + r16) * OROW + hf * 64 + g * 16 + i * 4);
-                        float4_t v = {o[hf * 4 + 0][mb][i] + z, o[hf * 4 + 1][mb][i] + z, o[hf * 4 + 2][mb][i] + z, o[hf * 4 + 3][mb][i] + z};
-                        v *= fac[mb];
-                        *p = w == 0 ? v : *p + v;
+                        float4_t *q = (float4_t *)(sums + (mb * 16 + r16) * OROW + hf * 64 + g * 16 + i * 4);
+                        const float4_t v = bt_channels<MB>(sum, mb, hf, i, z) * fac[mb];
+                        *q = w == 0 ? v : *q + v;
                     }
             }
         __syncthreads();
     }
-    const int64_t slot0 = ((int64_t)ch * a.heads + h) * mp + (int64_t)qb * 16 * MB;
+    const int64_t slot0 = ((int64_t)p.ch * a.heads + p.h) * a.mp[WHICH] + (int64_t)p.qb * 16 * MB;
     for (int i = tid; i < 16 * MB * 32; i += BT_NT) {
         const int row = i >> 5, c = (i & 31) * 4;
-        if (qb * 16 * MB + row < n_q) *(float4_t *)(a.w.part_o[WHICH] + (slot0 + row) * 128 + c) = *(const float4_t *)(sums + row * OROW + c);
+        if (p.qb * 16 * MB + row < p.n_q) *(float4_t *)(a.w.part_o[WHICH] + (slot0 + row) * 128 + c) = *(const float4_t *)(sums + row * OROW + c);
     }
-    if (tid < 16 * MB && qb * 16 * MB + tid < n_q) {
+    if (tid < 16 * MB && p.qb * 16 * MB + tid < p.n_q) {
         float m = KVQ_STAT_FLOOR, l = 0.0f;
         for (int w = 0; w < BT_WAVES; ++w) m = __builtin_fmaxf(m, wave_m[w][tid]);
         for (int w = 0; w < BT_WAVES; ++w) l += wave_l[w][tid] * __builtin_amdgcn_exp2f(wave_m[w][tid] - m - kap);
         *(float2_t *)(a.w.part_ml[WHICH] + (slot0 + tid) * 2) = float2_t{m, l};
     }
-    (void)n_chunks;
+}
+
+// Second kernel, more than 32 queries: a workgroup takes them 32 QW at a time and `chunk` blocks, in tiles of 64 tokens.  Each
+// wavefront rotates 16 tokens' Keys into LDS, in the operands' layout and in two parts; then it multiplies all 64 tokens (QW = 4), or 32 of
+// them (QW = 2), with 32 queries that it keeps in registers.  De-quantising is shared by 64 or 128 queries, and while one workgroup of a
+// compute unit does that (vector instructions) the other one's products keep the matrix cores busy.
+// The Keys' residuals are added where the rotated pairs lie, by a lane per entry: entries of channels below 64 first, so that two of
+// one pair never meet.
+template <int BITS, int QW, int WHICH>
+__global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
+{
+    constexpr int MB = 2, TW = BT_WAVES / QW, GROUPS = 2 / TW;        // blocks of 32 tokens that a wavefront multiplies per tile
+    constexpr int OROW = 132;
+    constexpr int KEYS = 4 * 4 * 2 * 1024;
+    static_assert(TW == 1 || QW * 32 * OROW * 4 <= KEYS + 2 * BT_PATCH, "the sums take the tiles' place");
+    __shared__ __attribute__((aligned(16))) uint8_t keys[KEYS + 2 * BT_PATCH];      // [block of 16][step t][part][lane]; residuals
+    __shared__ BtConst<BITS> con;
+    __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];
+    __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r16 = lane & 15, g = lane >> 4, qg = wave % QW, tg = wave / QW;
+    const BtPart p = bt_part<WHICH>(a, 32 * QW);
+    const BtSeg &sg = a.w.segs[p.si];
+    uint8_t *const patches = keys + KEYS;
+
+    con.stage(a, sg, p);
+    for (int i = tid; i < 2 * BT_PATCH / 16; i += BT_NT) *(uint4 *)(patches + i * 16) = uint4{0u, 0u, 0u, 0u};
+    const int q0 = (p.qb * QW + qg) * 32;
+    half8_t qf[MB][4][2];
+    BtSums<MB> sum;
+    sum.clear();
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const int row = q0 + mb * 16 + r16;
+        const bool in = row < p.n_q;
+        sum.inv[mb] = in ? a.w.row_scale[WHICH][p.row0 + row] : 0.0f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                uint4 v = {0u, 0u, 0u, 0u};
+                if (in) v = *(const uint4 *)(a.w.rows[WHICH] + (p.row0 + row) * BT_ROW + part * 128 + (t * 4 + g) * 8);
+                qf[mb][t][part] = __builtin_bit_cast(half8_t, v);
+            }
+    }
+    const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
+    const float my_vh = hdr->rope_vh[lane], my_vl = hdr->rope_vl[lane];
+    __syncthreads();
+    const float kap = con.kappa();
+    float minus_one = -1.0f;
+    asm("" : "+v"(minus_one));
+    const uint8_t *const k_plane = sg.k_codes + (int64_t)sg.cap * 16 * BITS * p.h, *const v_plane = sg.v_codes + (int64_t)sg.cap * 16 * BITS * p.h;
+    const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
+    const BtLane<BITS> my(r16, g);
+    const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
+
+    // Tiles of two blocks; the second one of the last may lie behind the tokens: it is read where the first is and has no weights.
+    const int tiles = (p.b1 - p.b0 + 1) / 2;
+    auto block_of = [&](int tile, int which) {
+        const int b = p.b0 + 2 * (tile < tiles ? tile : tiles - 1) + which;
+        return b < p.b1 ? b : p.b1 - 1;
+    };
+    const int mine = wave >> 1, half = wave & 1;                 // the block this wavefront rotates, and which half of it
+    auto place_of = [&](int tile) { return (int64_t)(sg.blk0 + block_of(tile, mine)) * (a.heads + 1) + p.h; };
+    uint32_t kw[BITS], ke = 0, ve = 0;
+    auto load_keys = [&](int tile) {
+        const int n0 = block_of(tile, mine) * BT_BLOCK + half * 16;
+        const uint8_t *kc = k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
+#pragma unroll
+        for (int i = 0; i < BITS; ++i) kw[i] = *(const uint32_t *)(kc + my.k_off[i]);
+    };
+    BtTable tab;
+    tab.load(a, place_of(lane));
+    BtPlaces at(tab, 0);
+    BtValues<BITS> val;
+    load_keys(0);
+    val.scales(sg.v_sz, block_of(0, tg) * BT_BLOCK, g);
+    val.codes(v_plane, v_half, block_of(0, tg) * BT_BLOCK, my);
+    if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
+    if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
+    uint8_t *const my_keys = keys + wave * 8192;
+    uint8_t *const my_patch = patches + mine * BT_PATCH;
+
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int next = tile + 1;
+        if ((next & 63) == 0) tab.load(a, place_of(next + lane));
+        const BtPlaces at_next(tab, next & 63);
+        // ---- this wavefront's 16 tokens
+        {
+            const int n0 = block_of(tile, mine) * BT_BLOCK + half * 16;
+            base[wave][lane] = rope_rev((float)n0, my_vh, my_vl);
+            bt_lds_order();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const uint4 sv = *(const uint4 *)&con.s[g * 16 + t * 4], zv = *(const uint4 *)&con.z[g * 16 + t * 4];
+                const float4_t vh = *(const float4_t *)&con.vh[g * 16 + t * 4], ba = *(const float4_t *)&base[wave][g * 16 + t * 4];
+                const uint32_t s4[4] = {sv.x, sv.y, sv.z, sv.w}, z4[4] = {zv.x, zv.y, zv.z, zv.w};
+                uint32_t kh[4], kl[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    bt_key_pair<false>(con.lut_k[bt_key_field<BITS>(kw, 4 * t + u)], s4[u], z4[u], 0u, __builtin_fmaf((float)r16, vh[u], ba[u]),
+                                       minus_one, 0.f, kh[u], kl[u]);
+                *(uint4 *)(my_keys + (t * 2 * 64 + lane) * 16) = uint4{kh[0], kh[1], kh[2], kh[3]};
+                *(uint4 *)(my_keys + ((t * 2 + 1) * 64 + lane) * 16) = uint4{kl[0], kl[1], kl[2], kl[3]};
+            }
+            bt_lds_order();
+            auto add_residual = [&](uint32_t x, bool upper) {
+                const uint32_t t = (x >> 7) & 31u, c = x & 127u, pr = c & 63u;
+                if ((int)(t >> 4) != half || (c >= 64u) != upper) return;
+                uint8_t *at_hi = my_keys + ((((pr >> 2) & 3) * 2 * 64 + (pr >> 4) * 16 + (t & 15)) * 4 + (pr & 3)) * 4;
+                const half2_t h2 = *(const half2_t *)at_hi, l2 = *(const half2_t *)(at_hi + 1024);
+                const float r = kvq_h2f((uint16_t)(x >> 16)), rev = __builtin_fmaf((float)(t & 15), con.vh[pr], base[wave][pr]);
+                const float c1 = __builtin_amdgcn_cosf(rev), s1 = __builtin_amdgcn_sinf(rev);
+                const float k0 = (float)h2.x + (float)l2.x, k1 = (float)h2.y + (float)l2.y;
+                uint32_t hi, lo;
+                bt_split(__builtin_fmaf(r, upper ? -s1 : c1, k0), __builtin_fmaf(r, upper ? c1 : s1, k1), minus_one, hi, lo);
+                *(uint32_t *)at_hi = hi;
+                *(uint32_t *)(at_hi + 1024) = lo;
+            };
+#pragma unroll
+            for (int upper = 0; upper < 2; ++upper) {
+                if (at.k0 + lane < at.k1) add_residual(ke, upper != 0);
+                for (uint32_t e = at.k0 + 64 + lane; e < at.k1; e += 64) add_residual(k_list[e], upper != 0);
+                bt_lds_order();
+            }
+        }
+        load_keys(next);
+        if (at_next.k0 + lane < at_next.k1) ke = k_list[at_next.k0 + lane];
+        const uint32_t vp = bt_value_place(ve);
+        const bool v_mine = at.v0 + lane < at.v1 && (int)((ve >> 11) & 1u) == half;
+        if (v_mine) *(uint16_t *)(my_patch + vp) = (uint16_t)(ve >> 16);
+        for (uint32_t e = at.v0 + 64 + lane; e < at.v1; e += 64) {
+            const uint32_t x = v_list[e];
+            if ((int)((x >> 11) & 1u) == half) *(uint16_t *)(my_patch + bt_value_place(x)) = (uint16_t)(x >> 16);
+        }
+        __syncthreads();
+        // ---- products with this wavefront's queries
+#pragma unroll
+        for (int gr = 0; gr < GROUPS; ++gr) {
+            const int grp = TW == 1 ? gr : tg, blk = p.b0 + 2 * tile + grp, n0 = blk * BT_BLOCK;
+            const bool edge = n0 < p.first || n0 + BT_BLOCK > p.n || blk >= p.b1;
+            const int blk_next = gr + 1 < GROUPS ? block_of(tile, gr + 1) : block_of(next, TW == 1 ? 0 : tg);
+            float4_t s[2][MB];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) s[tb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                half8_t hi[2], lo[2];
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
+                    const uint8_t *k = keys + (((grp * 2 + tb) * 4 + t) * 2 * 64 + lane) * 16;
+                    hi[tb] = *(const half8_t *)k;
+                    lo[tb] = *(const half8_t *)(k + 1024);
+                }
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) s[tb][mb] = bt_mfma(lo[tb], qf[mb][t][0], s[tb][mb]);
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) s[tb][mb] = bt_mfma(hi[tb], qf[mb][t][1], s[tb][mb]);
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) s[tb][mb] = bt_mfma(hi[tb], qf[mb][t][0], s[tb][mb]);
+            }
+            BtWeights w[MB];
+            bt_weights<BITS, MB>(s, val, sum, w, edge, n0, p.first, blk >= p.b1 ? 0 : p.n, g, r16, kap, minus_one);
+            val.scales(sg.v_sz, blk_next * BT_BLOCK, g);
+            bt_output<BITS, MB>(val, w, sum, con.lut_v, my.v_shift, patches + grp * BT_PATCH, lane);
+            val.codes(v_plane, v_half, blk_next * BT_BLOCK, my);
+        }
+        __syncthreads();
+        if (v_mine) *(uint16_t *)(my_patch + vp) = 0;
+        for (uint32_t e = at.v0 + 64 + lane; e < at.v1; e += 64) {
+            const uint32_t x = v_list[e];
+            if ((int)((x >> 11) & 1u) == half) *(uint16_t *)(my_patch + bt_value_place(x)) = 0;
+        }
+        if (at_next.v0 + lane < at_next.v1) ve = v_list[at_next.v0 + lane];
+        at = at_next;
+    }
+
+    // ---- sums to memory; with two wavefronts per query the second's go through LDS
+    const int64_t slot0 = ((int64_t)p.ch * a.heads + p.h) * a.mp[WHICH];
+    if (TW == 2) {
+        __syncthreads();
+        if (g == 0)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                wave_m[wave][mb * 16 + r16] = sum.m[mb];
+                wave_l[wave][mb * 16 + r16] = sum.lz[mb][1];
+            }
+        __syncthreads();
+    }
+    float *sums = (float *)keys + qg * 32 * OROW;
+#pragma unroll
+    for (int turn = 0; turn < TW; ++turn) {
+        // the second wavefront first, then the first adds its own and writes
+        if (TW == 1 || tg == 1 - turn) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                const int c = mb * 16 + r16;
+                float m = sum.m[mb], l = sum.lz[mb][1];
+                if (TW == 2) {
+                    m = __builtin_fmaxf(wave_m[qg][c], wave_m[(QW + qg) % BT_WAVES][c]);
+                    l = wave_l[qg][c] * __builtin_amdgcn_exp2f(wave_m[qg][c] - m) +
+                        wave_l[(QW + qg) % BT_WAVES][c] * __builtin_amdgcn_exp2f(wave_m[(QW + qg) % BT_WAVES][c] - m);
+                }
+                const float fac = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap), z = __shfl(sum.lz[mb][0], r16);
+                const bool in = q0 + c < p.n_q;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int ch = hf * 64 + g * 16 + i * 4;
+                        float4_t v = bt_channels<MB>(sum, mb, hf, i, z) * fac;
+                        float4_t *q = (float4_t *)(sums + c * OROW + ch);
+                        if (TW == 2 && turn == 0) *q = v;
+                        else {
+                            if (TW == 2) v += *q;
+                            if (in) *(float4_t *)(a.w.part_o[WHICH] + (slot0 + q0 + c) * 128 + ch) = v;
+                        }
+                    }
+                if ((TW == 1 || turn == 1) && g == 0 && in)
+                    *(float2_t *)(a.w.part_ml[WHICH] + (slot0 + q0 + c) * 2) = float2_t{m, l * __builtin_amdgcn_exp2f(-kap)};
+            }
+        }
+        if (TW == 2) __syncthreads();
+    }
 }
 
 // Third kernel: a workgroup per (sequence, query head) joins the workgroups' sums and the attention-sink tokens.  Eight slices of
@@ -775,7 +1112,8 @@ struct BtPlan {
 
 int64_t bt_up(int64_t n) { return (n + 255) & ~(int64_t)255; }
 
-int bt_mb(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : 4; }
+// Blocks of 16 queries that a workgroup takes: one or two, each of its wavefronts alone; four or eight, together.
+int bt_mb(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : queries <= 64 ? 4 : 8; }
 
 // The tokens of a call and the places of everything in the workspace (from `base`, which may be null).
 kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs, char *base, BtPlan &p)
@@ -870,7 +1208,8 @@ kvq_status bt_launch_bits(const BtArgs &a, int mb, hipStream_t s)
     const dim3 grid((unsigned)wgs), block(BT_NT);
     if (mb == 1) kvq_batch_attend<BITS, 1, WHICH><<<grid, block, 0, s>>>(a);
     else if (mb == 2) kvq_batch_attend<BITS, 2, WHICH><<<grid, block, 0, s>>>(a);
-    else kvq_batch_attend<BITS, 4, WHICH><<<grid, block, 0, s>>>(a);
+    else if (mb == 4) kvq_batch_team<BITS, 2, WHICH><<<grid, block, 0, s>>>(a);
+    else kvq_batch_team<BITS, 4, WHICH><<<grid, block, 0, s>>>(a);
     KVQ_HIP_CHECK(hipGetLastError());
     return KVQ_OK;
 }

@@ -130,6 +130,13 @@ def both(pairs, i):
     ("c2", dict(n_kv_heads=2, n_q_heads=2, outlier_fraction=0.0), 200, [10, 20], 0, False),
     ("c2", dict(n_kv_heads=8, n_q_heads=8), 2100, [3] * 40, 4, False),                     # 40 queries, prefix in several workgroups
     ("c2", dict(n_kv_heads=1, n_q_heads=2), 3, [2, 0], 4, False),                          # fewer tokens than sinks
+    # more than 32 queries of a KV head: tiles of 64 tokens shared by 64 or 128 of them
+    ("c2", dict(n_kv_heads=2, n_q_heads=16, bits=2), 385, [0, 9, 40, 1, 2], 2, False),     # 40, sinks, last tile of one token
+    ("c2", dict(n_kv_heads=1, n_q_heads=8, outlier_fraction=0.3), 290, [3] * 8, 0, False), # 64, more outliers than lanes
+    ("c2", dict(n_kv_heads=1, n_q_heads=9, outlier_fraction=0.2, bits=4), 225, [3] * 8, 1, True),   # 72, likewise, blocked storage
+    ("c4", dict(n_kv_heads=1, n_q_heads=8), 2500, [1] * 20, 0, False),                     # 160: two blocks of 128, many tiles
+    ("c2", dict(n_kv_heads=1, n_q_heads=70), 33, [65, 1], 0, False),                       # 70 of one sequence
+    ("c2", dict(n_kv_heads=2, n_q_heads=66, outlier_fraction=0.0), 64, [31, 0], 0, False), # 33 of one sequence, no outliers
 ])
 def test_batch_matches_the_definition(name, ov, prefix, own, sink, blocked):
     wl = S.workload(name, **ov)
