@@ -56,6 +56,7 @@ struct BtSeg {
     int32_t n, cap, shift, n_sink;
     int32_t blk0;                       // number of its first 32-token block
     int32_t chunk0;                     // number of its first workgroup's tokens among those of its launch
+    int32_t wg0, pad;                   // its first workgroup of the first kernel
 };
 
 struct BtWork {                         // the workspace
@@ -66,6 +67,7 @@ struct BtWork {                         // the workspace
     float *row_scale[2];
     uint32_t *k_list, *v_list;          // entries: residual << 16 | token << 7 | channel
     float *part_o[2], *part_ml[2];      // [chunk][head][query] sums of a workgroup: output; maximum, weights
+    int32_t *owner;                     // [chunk of own tokens]: whose
 };
 
 struct BtArgs {
@@ -79,101 +81,142 @@ struct BtArgs {
 
 struct BtSegs {
     BtSeg seg[BT_SEGS];
-    int32_t wg0[BT_SEGS + 1];                      // first workgroup of each
     int32_t first, n;                              // number of the first, how many
 };
 
 static_assert(sizeof(BtArgs) + sizeof(BtSegs) + 16 <= 4096, "kernel arguments");
 
+// A pointer that came out of memory, as one to global memory: the compiler takes it for one that may point to LDS as well, and loads
+// through such a pointer are waited for together with the LDS, the requests of the next step among them.  (Eight queries over
+// 131072 tokens, 32 heads: FLATUS us with such loads, GLOBALUS with these.)
+template <class T>
+__device__ __forceinline__ T *bt_global(T *p)
+{
+    return (T *)(__attribute__((address_space(1))) T *)(uintptr_t)p;
+}
+__device__ __forceinline__ BtSeg bt_seg(const BtSeg &g)
+{
+    BtSeg s = g;
+    s.k_codes = bt_global(g.k_codes); s.v_codes = bt_global(g.v_codes); s.v_sz = bt_global(g.v_sz);
+    s.k_ptr = bt_global(g.k_ptr); s.v_ptr = bt_global(g.v_ptr);
+    s.k_idx = bt_global(g.k_idx); s.k_val = bt_global(g.k_val); s.v_idx = bt_global(g.v_idx); s.v_val = bt_global(g.v_val);
+    s.params = bt_global(g.params); s.sink_k = bt_global(g.sink_k); s.sink_v = bt_global(g.sink_v);
+    return s;
+}
+
 template <bool BLOCKED>
 __device__ __forceinline__ uint32_t bt_entry(const void *arr, int shift, uint32_t e)
 {
     if (!BLOCKED) return ((const uint16_t *)arr)[e];
-    return ((const uint16_t *const *)arr)[e >> shift][e & ((1u << shift) - 1u)];
+    return bt_global(((const uint16_t *const *)arr)[e >> shift])[e & ((1u << shift) - 1u)];
 }
 
-// The entries of 32 tokens sorted by head: eight lanes a token, each entry's rank among its head's from the count it adds to, then
-// its place.  (The order within a head is any: every entry has an element of its own.)  A lane keeps up to BT_HELD entries in
-// registers from the count to the placing; tokens with more (over 48) are read twice instead.
-constexpr int BT_HELD = 6;
+// The entries of four blocks of 32 tokens sorted by block and head: eight lanes a token, an entry's rank among its head's from the count
+// that it adds to, its place from the sums of the counts.  (The order within a head is any: every entry has an element of its own.)
+// A lane keeps up to BT_HELD entries of each block in registers from the count to the placing; where a token has more (over 48)
+// they are read twice.  Each stage is a round trip to memory, so the four blocks go through them together (one block per
+// workgroup: 46 us over 48 sequences of 9000 tokens, 29 with four).  The sorted entries leave through LDS: stored straight to their
+// places, a line each, they take 45 us over 131072 tokens of 32 heads (ONEUS so).
+constexpr int BT_HELD = 6, BT_SORT = 4, BT_STAGE = BT_SORT * BT_BLOCK * 8 * BT_HELD;
 
 template <bool BLOCKED>
 __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int n,
-                             int heads, uint32_t *start, uint32_t *list, uint32_t *count)
+                             int heads, uint32_t *start, uint32_t *list, uint32_t *count, uint32_t *stage)
 {
-    const int tid = threadIdx.x, t = tid >> 3, l = tid & 7;
-    for (int h = tid; h < heads; h += BT_NT) count[h] = 0u;
-    uint32_t p0 = 0, p1 = 0;
-    if (n0 + t < n) {
-        p0 = ptr[n0 + t];
-        p1 = ptr[n0 + t + 1];
-        p1 = p1 < room ? p1 : room;
-    }
-    const uint32_t base = ptr[n0];
-    uint32_t ch[BT_HELD], x[BT_HELD], rank[BT_HELD];
+    const int tid = threadIdx.x, t = tid >> 3, l = tid & 7, lane = tid & 63, wave = tid >> 6;
+    for (int h = tid; h < BT_SORT * heads; h += BT_NT) count[h] = 0u;
+    uint32_t p0[BT_SORT], p1[BT_SORT], x[BT_SORT][BT_HELD], rank[BT_SORT][BT_HELD];
+    const int my_first = n0 + wave * BT_BLOCK;                   // first token of the block whose sums this wavefront takes
+    const uint32_t base = my_first < n ? ptr[my_first] : 0u, all0 = ptr[n0];
 #pragma unroll
-    for (int i = 0; i < BT_HELD; ++i) {
-        const uint32_t e = p0 + l + 8 * i;
-        ch[i] = 0xFFFFFFFFu;
-        if (e < p1) {
-            ch[i] = bt_entry<BLOCKED>(idx, shift, e);
-            x[i] = bt_entry<BLOCKED>(val, shift, e);
+    for (int b = 0; b < BT_SORT; ++b) {
+        const int m = n0 + b * BT_BLOCK + t;
+        p0[b] = ptr[m < n ? m : n];
+        p1[b] = ptr[m < n ? m + 1 : n];
+    }
+    bool more = false;
+#pragma unroll
+    for (int b = 0; b < BT_SORT; ++b) {
+        p1[b] = p1[b] < room ? p1[b] : room;
+        more |= p1[b] > p0[b] + 8 * BT_HELD;
+#pragma unroll
+        for (int i = 0; i < BT_HELD; ++i) {
+            const uint32_t e = p0[b] + l + 8 * i;
+            if (e < p1[b]) x[b][i] = bt_entry<BLOCKED>(idx, shift, e) | (bt_entry<BLOCKED>(val, shift, e) << 16);
         }
     }
-    const bool many = __syncthreads_or(p1 > p0 && p1 - p0 > 8 * BT_HELD) != 0;
-    if (!many) {
+    const bool many = __syncthreads_or(more) != 0;
 #pragma unroll
-        for (int i = 0; i < BT_HELD; ++i)
-            if ((ch[i] >> 7) < (uint32_t)heads) rank[i] = atomicAdd(&count[ch[i] >> 7], 1u);
-    } else {
-        for (uint32_t e = p0 + l; e < p1; e += 8) {
-            const uint32_t h = bt_entry<BLOCKED>(idx, shift, e) >> 7;
-            if (h < (uint32_t)heads) atomicAdd(&count[h], 1u);
+    for (int b = 0; b < BT_SORT; ++b) {
+        uint32_t *const mine = count + b * heads;
+        if (!many) {
+#pragma unroll
+            for (int i = 0; i < BT_HELD; ++i)
+                if (p0[b] + l + 8 * i < p1[b] && ((x[b][i] & 0xFFFFu) >> 7) < (uint32_t)heads) rank[b][i] = atomicAdd(&mine[(x[b][i] & 0xFFFFu) >> 7], 1u);
+        } else {
+            for (uint32_t e = p0[b] + l; e < p1[b]; e += 8) {
+                const uint32_t h = bt_entry<BLOCKED>(idx, shift, e) >> 7;
+                if (h < (uint32_t)heads) atomicAdd(&mine[h], 1u);
+            }
         }
     }
     __syncthreads();
-    if (tid < 64) {                                 // exclusive sums, up to eight heads a lane
-        uint32_t c[BT_MAX_HEADS / 64], s = 0;
+    {                                               // exclusive sums, a wavefront a block, up to eight heads a lane
+        static_assert(BT_SORT == BT_WAVES, "a wavefront per block");
+        uint32_t c[BT_MAX_HEADS / 64], s = 0, *const mine = count + wave * heads;
         const int per = (heads + 63) / 64;
 #pragma unroll
         for (int i = 0; i < BT_MAX_HEADS / 64; ++i) {
-            const int h = tid * per + i;
-            c[i] = (i < per && h < heads) ? count[h] : 0u;
+            const int h = lane * per + i;
+            c[i] = (i < per && h < heads) ? mine[h] : 0u;
             s += c[i];
         }
         uint32_t before = s;
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = (uint32_t)__shfl_up((int)before, d);
-            if (tid >= d) before += o;
+            if (lane >= d) before += o;
         }
-        before -= s;
+        before += base - s;
 #pragma unroll
         for (int i = 0; i < BT_MAX_HEADS / 64; ++i) {
-            const int h = tid * per + i;
+            const int h = lane * per + i;
             if (i < per && h < heads) {
-                count[h] = base + before;
-                start[h] = base + before;
+                mine[h] = before;
+                if (my_first < n) {
+                    start[wave * (heads + 1) + h] = before;
+                    if (h == heads - 1) start[wave * (heads + 1) + heads] = before + c[i];
+                }
                 before += c[i];
-                if (h == heads - 1) start[heads] = base + before;
             }
         }
     }
     __syncthreads();
-    if (!many) {
 #pragma unroll
-        for (int i = 0; i < BT_HELD; ++i)
-            if ((ch[i] >> 7) < (uint32_t)heads) {
-                const uint32_t at = count[ch[i] >> 7] + rank[i];
-                if (at < room) list[at] = (x[i] << 16) | ((uint32_t)t << 7) | (ch[i] & 127u);
+    for (int b = 0; b < BT_SORT; ++b) {
+        uint32_t *const mine = count + b * heads;
+        if (!many) {
+#pragma unroll
+            for (int i = 0; i < BT_HELD; ++i) {
+                const uint32_t c = x[b][i] & 0xFFFFu;
+                if (p0[b] + l + 8 * i < p1[b] && (c >> 7) < (uint32_t)heads) {
+                    const uint32_t at = mine[c >> 7] + rank[b][i] - all0;
+                    if (at < (uint32_t)BT_STAGE) stage[at] = (x[b][i] & 0xFFFF0000u) | ((uint32_t)t << 7) | (c & 127u);
+                }
             }
-    } else {
-        for (uint32_t e = p0 + l; e < p1; e += 8) {
-            const uint32_t c = bt_entry<BLOCKED>(idx, shift, e), h = c >> 7;
-            if (h < (uint32_t)heads) {
-                const uint32_t at = atomicAdd(&count[h], 1u);
-                if (at < room) list[at] = (bt_entry<BLOCKED>(val, shift, e) << 16) | ((uint32_t)t << 7) | (c & 127u);
+        } else {
+            for (uint32_t e = p0[b] + l; e < p1[b]; e += 8) {
+                const uint32_t c = bt_entry<BLOCKED>(idx, shift, e);
+                if ((c >> 7) < (uint32_t)heads) {
+                    const uint32_t at = atomicAdd(&mine[c >> 7], 1u);
+                    if (at < room) list[at] = (bt_entry<BLOCKED>(val, shift, e) << 16) | ((uint32_t)t << 7) | (c & 127u);
+                }
             }
         }
+    }
+    if (!many) {
+        __syncthreads();
+        const uint32_t all = ptr[n0 + BT_SORT * BT_BLOCK < n ? n0 + BT_SORT * BT_BLOCK : n], end = all < room ? all : room;
+        for (uint32_t i = tid; all0 + i < end; i += BT_NT) list[all0 + i] = stage[i];
     }
 }
 
@@ -208,47 +251,62 @@ __device__ void bt_query_row(const BtArgs &a, const KvqParamsHeader *hdr, int wh
     if (lane == 0) a.w.row_scale[which][at] = ldexpf(1.0f, e - 14);
 }
 
-// First kernel: descriptors from the arguments to memory, outliers by head, query rows.
-__global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, int row_wgs)
+// Descriptors from the arguments to memory.
+__device__ __forceinline__ void bt_upload(const BtArgs &a, const BtSegs &s)
 {
-    __shared__ uint32_t count[BT_MAX_HEADS];
-    const int tid = threadIdx.x;
+    const uint32_t *from = (const uint32_t *)s.seg;
+    uint32_t *to = (uint32_t *)(a.w.segs + s.first);
+    for (int i = threadIdx.x; i < s.n * (int)(sizeof(BtSeg) / 4); i += BT_NT) to[i] = from[i];
+}
+__global__ __launch_bounds__(BT_NT) void kvq_batch_upload(BtArgs a, BtSegs s) { bt_upload(a, s); }
+
+// First kernel: query rows; outliers by head, BT_SORT blocks of 32 tokens and a side per workgroup.  A call whose descriptors fit in the
+// arguments brings them along; otherwise (`total` > s.n) they are in memory already.
+__global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, int row_wgs, int total)
+{
+    __shared__ uint32_t count[BT_SORT * BT_MAX_HEADS], stage[BT_STAGE];
+    const int tid = threadIdx.x, lane = tid & 63;
     int wg = blockIdx.x;
-    if (wg == 0) {
-        const BtSeg *from = s.seg;
-        uint32_t *to = (uint32_t *)(a.w.segs + s.first);
-        const int words = s.n * (int)(sizeof(BtSeg) / 4);
-        for (int i = tid; i < words; i += BT_NT) to[i] = ((const uint32_t *)from)[i];
-    }
+    if (wg == 0 && total == s.n) bt_upload(a, s);
     if (wg < row_wgs) {
-        const int rows = a.n_seqs * a.heads * a.ratio, wave = tid >> 6;
-        const int row = wg * BT_WAVES + wave;
+        const int rows = a.n_seqs * a.heads * a.ratio, row = wg * BT_WAVES + (tid >> 6);
         if (row >= rows) return;
-        const KvqParamsHeader *hdr = (const KvqParamsHeader *)s.seg[s.n - 1].params;       // the rotary constants are one layer's
-        if (a.prefix > 0) bt_query_row(a, hdr, 0, row, tid & 63);
-        if (a.own) bt_query_row(a, hdr, 1, row, tid & 63);
+        const KvqParamsHeader *hdr = (const KvqParamsHeader *)bt_global(s.seg[0].params);       // the rotary constants are one layer's
+        if (a.prefix > 0) bt_query_row(a, hdr, 0, row, lane);
+        if (a.own) bt_query_row(a, hdr, 1, row, lane);
         return;
     }
     wg -= row_wgs;
     const bool values = wg & 1;                     // a workgroup per side: the chain of each is latency
     wg >>= 1;
     int i = 0;
-    while (i + 1 < s.n && wg >= s.wg0[i + 1]) ++i;
-    const BtSeg &g = s.seg[i];
-    const int blk = wg - s.wg0[i], n0 = blk * BT_BLOCK;
+    if (total == s.n) {
+        while (i + 1 < s.n && wg >= s.seg[i + 1].wg0) ++i;
+    } else {                                        // the last whose first workgroup is not after this one
+        int found = 0;
+        for (int b = 0; b < total; b += 64) {
+            const int k = b + lane;
+            found += __popcll(__ballot(k < total && a.w.segs[k].wg0 <= wg));
+        }
+        i = __builtin_amdgcn_readfirstlane(found) - 1;
+    }
+    const BtSeg g = total == s.n ? bt_seg(s.seg[i]) : bt_seg(a.w.segs[i]);
+    const int blk = BT_SORT * (wg - g.wg0), n0 = blk * BT_BLOCK;
     if (n0 >= g.n) return;
     const int64_t at = (int64_t)(g.blk0 + blk) * (a.heads + 1);
     const uint32_t *ptr = values ? g.v_ptr : g.k_ptr;
     const void *idx = values ? g.v_idx : g.k_idx, *val = values ? g.v_val : g.k_val;
     const uint32_t room = values ? g.v_room : g.k_room;
+    if (blk == 0 && values && i > 0)                // the workgroups of a sequence's own tokens find it by their number
+        for (int c = tid; c < (g.n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK); c += BT_NT) a.w.owner[g.chunk0 + c] = i;
     uint32_t *start = (values ? a.w.v_start : a.w.k_start) + at, *list = values ? a.w.v_list + g.v_list : a.w.k_list + g.k_list;
-    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n, a.heads, start, list, count);
-    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n, a.heads, start, list, count);
-    if (values && tid < 64) {
+    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n, a.heads, start, list, count, stage);
+    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n, a.heads, start, list, count, stage);
+    if (values && tid < BT_SORT * BT_BLOCK) {
         float m = 0.0f;
-        if (tid < BT_BLOCK && n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
-        m = kvq_wave_max(m);
-        if (tid == 0) a.w.smax[g.blk0 + blk] = m;
+        if (n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
+        for (int d = 16; d; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+        if ((tid & 31) == 0 && n0 + tid < g.n) a.w.smax[g.blk0 + blk + (tid >> 5)] = m;
     }
 }
 
@@ -320,16 +378,7 @@ __device__ __forceinline__ BtPart bt_part(const BtArgs &a, int queries)
     p.qb = blockIdx.x % qblocks;
     p.h = (blockIdx.x / qblocks) % a.heads;
     p.ch = blockIdx.x / (qblocks * a.heads);
-    p.si = 0;
-    if (WHICH == 1) {                                      // the last sequence whose first chunk is not after this one
-        int lo = 1, hi = a.n_seqs + 1;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.w.segs[mid].chunk0 <= p.ch) lo = mid;
-            else hi = mid;
-        }
-        p.si = lo;
-    }
+    p.si = WHICH == 1 ? a.w.owner[p.ch] : 0;
     const BtSeg &sg = a.w.segs[p.si];
     p.n = sg.n;
     const int n_blocks = (p.n + BT_BLOCK - 1) / BT_BLOCK;
@@ -395,49 +444,54 @@ struct BtLane {
     }
 };
 
-// Values of 32 tokens as they are loaded: codes and (scale, zero-point) of this lane's channels and tokens.
+// The dwords with this lane's four fields of a half of 32 tokens' Values: [token block][pair].
 template <int BITS>
-struct BtValues {
-    uint32_t c0[2][2][2], c1[BITS == 3 ? 2 : 1][2][2];     // [half][token block][pair]: the dwords with four fields
-    uint32_t sz[2][4];
-    __device__ __forceinline__ void codes(const uint8_t *plane, int64_t half, int n0, const BtLane<BITS> &l)
+struct BtCodes {
+    uint32_t c0[2][2], c1[BITS == 3 ? 2 : 1][2];
+    __device__ __forceinline__ void load(const uint8_t *half, int n0, const BtLane<BITS> &l)
     {
-        const uint8_t *vc = plane + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
+        const uint8_t *vc = half + (int64_t)(n0 >> 7) * (64 * 16 * BITS) + ((n0 >> 1) & 63) * 16;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
+        for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int pr = 0; pr < 2; ++pr) {
-                    const uint8_t *p = vc + hf * half + tb * 128 + pr * 16;
-                    c0[hf][tb][pr] = *(const uint32_t *)(p + l.v_off0);
-                    if (BITS == 3) c1[hf][tb][pr] = *(const uint32_t *)(p + l.v_off1);
-                }
+            for (int pr = 0; pr < 2; ++pr) {
+                const uint8_t *p = vc + tb * 128 + pr * 16;
+                c0[tb][pr] = *(const uint32_t *)(p + l.v_off0);
+                if (BITS == 3) c1[tb][pr] = *(const uint32_t *)(p + l.v_off1);
+            }
     }
-    __device__ __forceinline__ void scales(const uint32_t *v_sz, int n0, int g)
+    // The fields at the bottom of a word each.
+    __device__ __forceinline__ void align(uint32_t (&w)[4], uint32_t shift) const
     {
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb) {
-            const uint4 v = *(const uint4 *)(v_sz + n0 + tb * 16 + g * 4);
-            sz[tb][0] = v.x; sz[tb][1] = v.y; sz[tb][2] = v.z; sz[tb][3] = v.w;
-        }
-    }
-    // Operand of channel block cb: channels 64 (cb / 4) + 4 r16 + cb % 4.
-    __device__ __forceinline__ half8_t operand(int cb, const uint32_t *lut, uint32_t shift) const
-    {
-        uint32_t x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint32_t w = c0[cb >> 2][i >> 1][i & 1];
-            if (BITS == 3) w = __builtin_amdgcn_alignbit(c1[BITS == 3 ? cb >> 2 : 0][i >> 1][i & 1], w, shift);
-            if (BITS == 2) w >>= shift;
-            const int sh = 2 * BITS * (cb & 3) - 2;
-            const uint32_t off = (sh < 0 ? w << -sh : w >> sh) & (((1u << 2 * BITS) - 1u) << 2);
-            x[i] = *(const uint32_t *)((const uint8_t *)lut + off);
+            w[i] = c0[i >> 1][i & 1];
+            if (BITS == 3) w[i] = __builtin_amdgcn_alignbit(c1[BITS == 3 ? i >> 1 : 0][i & 1], w[i], shift);
+            if (BITS == 2) w[i] >>= shift;
         }
-        return bt_half8(x[0], x[1], x[2], x[3]);
     }
 };
+// Operand of one of the half's channel blocks: channels 4 r16 + sub of the half.
+template <int BITS>
+__device__ __forceinline__ half8_t bt_value_operand(const uint32_t (&w)[4], int sub, const uint32_t *lut)
+{
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int sh = 2 * BITS * sub - 2;
+        x[i] = *(const uint32_t *)((const uint8_t *)lut + ((sh < 0 ? w[i] << -sh : w[i] >> sh) & (((1u << 2 * BITS) - 1u) << 2)));
+    }
+    return bt_half8(x[0], x[1], x[2], x[3]);
+}
+// (scale, zero-point) of this lane's tokens: 4 g .. 4 g + 3 of both blocks.
+__device__ __forceinline__ void bt_scales(uint32_t (&sz)[2][4], const uint32_t *v_sz, int n0, int g)
+{
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+        const uint4 v = *(const uint4 *)(v_sz + n0 + tb * 16 + g * 4);
+        sz[tb][0] = v.x; sz[tb][1] = v.y; sz[tb][2] = v.z; sz[tb][3] = v.w;
+    }
+}
 
 // One pair (i, i + 64) of a token: de-quantised, its residuals added, rotated, in two parts.
 template <bool PATCHED>
@@ -484,37 +538,53 @@ struct BtWeights {                      // p and p s in two parts
     half8_t ph, pl, wh, wl;
 };
 
-// Scores of 32 tokens from n0 on to weights; tokens outside [first, n) have none.
-template <int BITS, int MB>
-__device__ __forceinline__ void bt_weights(float4_t (&s)[2][MB], BtValues<BITS> &v, BtSums<MB> &sum, BtWeights (&w)[MB], bool edge, int n0,
-                                           int first, int n, int g, int r16, float kap, float minus_one)
+// Tokens outside [first, n) of the 32 from n0 on get no weight.
+template <int MB>
+__device__ __forceinline__ void bt_mask(float4_t (&s)[2][MB], uint32_t (&sz)[2][4], int n0, int first, int n, int g)
 {
-    if (edge) {
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = n0 + tb * 16 + g * 4 + i;
+            const bool in = t >= first && t < n;
+            if (!in) sz[tb][i] = 0u;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+                if (!in) s[tb][mb][i] = -__builtin_inff();
+        }
+}
+
+// The running maximum of block mb's queries over GROUPS x 32 more scores; where it grows by much (2^BT_MAX_SLACK in the weights) the sums
+// move to the new one.
+template <int MB, int GROUPS>
+__device__ __forceinline__ void bt_maximum(const float4_t (&s)[GROUPS][2][MB], BtSums<MB> &sum, int mb)
+{
+    float m = s[0][0][mb][0];
+#pragma unroll
+    for (int gr = 0; gr < GROUPS; ++gr)
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = n0 + tb * 16 + g * 4 + i;
-                const bool in = t >= first && t < n;
-                if (!in) v.sz[tb][i] = 0u;
+            for (int i = 0; i < 4; ++i) m = __builtin_fmaxf(m, s[gr][tb][mb][i]);
+    m = bt_column_max(m) * sum.inv[mb];
+    if (!(m >= KVQ_STAT_FLOOR)) m = KVQ_STAT_FLOOR;          // no token at all (-inf, or -inf * 0 in a column without a query)
+    if (__ballot(m > sum.m[mb] + BT_MAX_SLACK) != 0ull) {
+        const float up = m > sum.m[mb] ? m : sum.m[mb], f = __builtin_amdgcn_exp2f(sum.m[mb] - up);
+        sum.m[mb] = up;
+        sum.lz[mb] *= f;
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
-                    if (!in) s[tb][mb][i] = -__builtin_inff();
-            }
+        for (int cb = 0; cb < 8; ++cb) sum.o[cb][mb] *= f;
     }
+}
+
+// Scores of 32 tokens to weights, and the sums of p z and of p (a channel block of their own with rows (z, 1, 0 ...)).
+template <int MB>
+__device__ __forceinline__ void bt_weights(const float4_t (&s)[2][MB], const uint32_t (&sz)[2][4], BtSums<MB> &sum, BtWeights (&w)[MB], int r16,
+                                           float kap, float minus_one)
+{
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
-        float m = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[0][mb][0], s[0][mb][1]), __builtin_fmaxf(s[0][mb][2], s[0][mb][3])),
-                                  __builtin_fmaxf(__builtin_fmaxf(s[1][mb][0], s[1][mb][1]), __builtin_fmaxf(s[1][mb][2], s[1][mb][3])));
-        m = bt_column_max(m) * sum.inv[mb];
-        if (!(m >= KVQ_STAT_FLOOR)) m = KVQ_STAT_FLOOR;      // no token of the block (-inf, or -inf * 0 in a column without a query)
-        if (__ballot(m > sum.m[mb] + BT_MAX_SLACK) != 0ull) {
-            const float up = m > sum.m[mb] ? m : sum.m[mb], f = __builtin_amdgcn_exp2f(sum.m[mb] - up);
-            sum.m[mb] = up;
-            sum.lz[mb] *= f;
-#pragma unroll
-            for (int cb = 0; cb < 8; ++cb) sum.o[cb][mb] *= f;
-        }
         const float shift = kap - sum.m[mb];
         uint32_t a_h[4], a_l[4], w_h[4], w_l[4];
 #pragma unroll
@@ -523,7 +593,7 @@ __device__ __forceinline__ void bt_weights(float4_t (&s)[2][MB], BtValues<BITS> 
             for (int i = 0; i < 4; i += 2) {
                 const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i], sum.inv[mb], shift));
                 const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][mb][i + 1], sum.inv[mb], shift));
-                const float s0 = (float)__builtin_bit_cast(half2_t, v.sz[tb][i]).x, s1 = (float)__builtin_bit_cast(half2_t, v.sz[tb][i + 1]).x;
+                const float s0 = (float)__builtin_bit_cast(half2_t, sz[tb][i]).x, s1 = (float)__builtin_bit_cast(half2_t, sz[tb][i + 1]).x;
                 bt_split(p0, p1, minus_one, a_h[tb * 2 + i / 2], a_l[tb * 2 + i / 2]);
                 bt_split(p0 * s0, p1 * s1, minus_one, w_h[tb * 2 + i / 2], w_l[tb * 2 + i / 2]);
             }
@@ -532,11 +602,10 @@ __device__ __forceinline__ void bt_weights(float4_t (&s)[2][MB], BtValues<BITS> 
         w[mb].wh = bt_half8(w_h[0], w_h[1], w_h[2], w_h[3]);
         w[mb].wl = bt_half8(w_l[0], w_l[1], w_l[2], w_l[3]);
     }
-    // sum of p z and sum of p: a channel block of its own with rows (z, 1, 0 ...)
     uint32_t x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t z2 = __builtin_amdgcn_perm(v.sz[i >> 1][(i & 1) * 2 + 1], v.sz[i >> 1][(i & 1) * 2], 0x07060302u);
+        const uint32_t z2 = __builtin_amdgcn_perm(sz[i >> 1][(i & 1) * 2 + 1], sz[i >> 1][(i & 1) * 2], 0x07060302u);
         x[i] = r16 == 0 ? z2 : r16 == 1 ? 0x3C003C00u : 0u;
     }
     const half8_t zf = bt_half8(x[0], x[1], x[2], x[3]);
@@ -547,23 +616,18 @@ __device__ __forceinline__ void bt_weights(float4_t (&s)[2][MB], BtValues<BITS> 
     }
 }
 
-// The output's products of 32 tokens; `patch` holds their residuals.
-template <int BITS, int MB>
-__device__ __forceinline__ void bt_output(const BtValues<BITS> &v, const BtWeights (&w)[MB], BtSums<MB> &sum, const uint32_t *lut_v,
-                                          uint32_t v_shift, const uint8_t *patch, int lane)
+// The output's products with one block of channels: `vf` its signposts, `rf` its residuals.
+template <int MB>
+__device__ __forceinline__ void bt_products(half8_t vf, half8_t rf, const BtWeights (&w)[MB], BtSums<MB> &sum, int cb)
 {
 #pragma unroll
-    for (int cb = 0; cb < 8; ++cb) {
-        const half8_t vf = v.operand(cb, lut_v, v_shift);
-        const half8_t rf = *(const half8_t *)(patch + (cb * 64 + lane) * 16);
+    for (int mb = 0; mb < MB; ++mb) sum.o[cb][mb] = bt_mfma(rf, w[mb].pl, sum.o[cb][mb]);
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-            sum.o[cb][mb] = bt_mfma(rf, w[mb].pl, sum.o[cb][mb]);
-            sum.o[cb][mb] = bt_mfma(vf, w[mb].wl, sum.o[cb][mb]);
-            sum.o[cb][mb] = bt_mfma(rf, w[mb].ph, sum.o[cb][mb]);
-            sum.o[cb][mb] = bt_mfma(vf, w[mb].wh, sum.o[cb][mb]);
-        }
-    }
+    for (int mb = 0; mb < MB; ++mb) sum.o[cb][mb] = bt_mfma(vf, w[mb].wl, sum.o[cb][mb]);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) sum.o[cb][mb] = bt_mfma(rf, w[mb].ph, sum.o[cb][mb]);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) sum.o[cb][mb] = bt_mfma(vf, w[mb].wh, sum.o[cb][mb]);
 }
 
 // Four consecutive channels (64 hf + 16 g + 4 i ..) of block mb's query of this lane, with the zero-points' part.
@@ -598,9 +662,8 @@ template <int BITS, int MB, int WHICH>
 __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArgs a)
 {
     constexpr int QBYTES = 8192 * MB;
-    constexpr int OROW = 132;                              // floats of a query's row of sums (padded)
-    constexpr int SUMS = 16 * MB * OROW * 4, PATCHES = BT_WAVES * BT_PATCH;
-    static_assert(SUMS <= PATCHES, "the sums take the patches' place");
+    constexpr int PATCHES = BT_WAVES * BT_PATCH;
+    static_assert(16 * 128 * 4 == BT_PATCH, "the sums of 16 queries take a patch's place");
     __shared__ __attribute__((aligned(16))) uint8_t area[PATCHES];
     __shared__ __attribute__((aligned(16))) uint8_t qfrag[QBYTES];
     __shared__ BtConst<BITS> con;
@@ -610,8 +673,38 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const BtPart p = bt_part<WHICH>(a, 16 * MB);
-    const BtSeg &sg = a.w.segs[p.si];
+    const BtSeg sg = bt_seg(a.w.segs[p.si]);
 
+    uint8_t *const patch = area + wave * BT_PATCH;
+    const uint8_t *const k_plane = sg.k_codes + (int64_t)sg.cap * 16 * BITS * p.h, *const v_plane = sg.v_codes + (int64_t)sg.cap * 16 * BITS * p.h;
+    const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
+    const BtLane<BITS> my(r16, g);
+
+    // What a step reads is requested by the step before, as soon as the registers it lands in are free: codes of the Keys after
+    // the scores, scales after the weights, codes of the Values after the output's products, a list's entries (one a lane; lists
+    // of more go on from memory) after the patch has been zeroed.  (Eight queries, 131072 tokens, 32 heads: 381 -> 302 us.)
+    const int steps = p.b1 - p.b0 > wave ? (p.b1 - p.b0 - wave + BT_WAVES - 1) / BT_WAVES : 0;
+    const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
+    uint32_t kw[2][BITS], ke = 0, ve = 0, sz[2][4];
+    BtCodes<BITS> vc[2];
+    BtTable tab = {0, 0, 0, 0};
+    auto block_of = [&](int step) { return p.b0 + wave + BT_WAVES * (step < steps ? step : steps - 1); };
+    auto place_of = [&](int step) { return (int64_t)(sg.blk0 + block_of(step)) * (a.heads + 1) + p.h; };
+    auto load_keys = [&](int n0) {
+        const uint8_t *kc = k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int i = 0; i < BITS; ++i) kw[tb][i] = *(const uint32_t *)(kc + my.k_off[i] + tb * 256);
+    };
+    if (steps > 0) {
+        const int n0 = block_of(0) * BT_BLOCK;
+        tab.load(a, place_of(lane));
+        load_keys(n0);
+        bt_scales(sz, sg.v_sz, n0, g);
+        vc[0].load(v_plane, n0, my);
+        vc[1].load(v_plane + v_half, n0, my);
+    }
     con.stage(a, sg, p);
 #pragma unroll
     for (int i = tid; i < QBYTES / 16; i += BT_NT) {
@@ -631,42 +724,13 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
         const int row = (p.qb * MB + mb) * 16 + r16;
         sum.inv[mb] = row < p.n_q ? a.w.row_scale[WHICH][p.row0 + row] : 0.0f;
     }
+    BtPlaces at(tab, 0);
+    if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
+    if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
     __syncthreads();
     const float kap = con.kappa();
     float minus_one = -1.0f, one = 1.0f;
     asm("" : "+v"(minus_one), "+v"(one));
-    uint8_t *const patch = area + wave * BT_PATCH;
-    const uint8_t *const k_plane = sg.k_codes + (int64_t)sg.cap * 16 * BITS * p.h, *const v_plane = sg.v_codes + (int64_t)sg.cap * 16 * BITS * p.h;
-    const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
-    const BtLane<BITS> my(r16, g);
-
-    // What a step reads is requested by the step before, as soon as the registers it lands in are free: codes of the Keys after
-    // the scores, scales after the weights, codes of the Values after the output's products, a list's entries (one a lane; lists
-    // of more go on from memory) after the patch has been zeroed.  (Eight queries, 131072 tokens, 32 heads: 381 -> 302 us.)
-    const int steps = p.b1 - p.b0 > wave ? (p.b1 - p.b0 - wave + BT_WAVES - 1) / BT_WAVES : 0;
-    const uint32_t *k_list = a.w.k_list + sg.k_list, *v_list = a.w.v_list + sg.v_list;
-    uint32_t kw[2][BITS], ke = 0, ve = 0;
-    BtValues<BITS> val;
-    BtTable tab = {0, 0, 0, 0};
-    auto block_of = [&](int step) { return p.b0 + wave + BT_WAVES * (step < steps ? step : steps - 1); };
-    auto place_of = [&](int step) { return (int64_t)(sg.blk0 + block_of(step)) * (a.heads + 1) + p.h; };
-    auto load_keys = [&](int n0) {
-        const uint8_t *kc = k_plane + (int64_t)(n0 >> 6) * (64 * 16 * BITS) + (n0 & 63) * 16;
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-            for (int i = 0; i < BITS; ++i) kw[tb][i] = *(const uint32_t *)(kc + my.k_off[i] + tb * 256);
-    };
-    if (steps > 0) {
-        const int n0 = block_of(0) * BT_BLOCK;
-        tab.load(a, place_of(lane));
-        load_keys(n0);
-        val.scales(sg.v_sz, n0, g);
-        val.codes(v_plane, v_half, n0, my);
-    }
-    BtPlaces at(tab, 0);
-    if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
-    if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
 
     for (int step = 0; step < steps; ++step) {
         const int n0 = block_of(step) * BT_BLOCK, next = step + 1, n0_next = block_of(next) * BT_BLOCK;
@@ -683,7 +747,7 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
             *(uint16_t *)(patch + bt_key_place(x)) = (uint16_t)(x >> 16);
         }
         bt_lds_order();
-        float4_t s[2][MB];
+        float4_t sc[1][2][MB], (&s)[2][MB] = sc[0];
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -732,11 +796,22 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
             *(uint16_t *)(patch + bt_value_place(x)) = (uint16_t)(x >> 16);
         }
         BtWeights w[MB];
-        bt_weights<BITS, MB>(s, val, sum, w, edge, n0, p.first, p.n, g, r16, kap, minus_one);
-        val.scales(sg.v_sz, n0_next, g);
+        if (edge) bt_mask<MB>(s, sz, n0, p.first, p.n, g);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) bt_maximum<MB, 1>(sc, sum, mb);
+        bt_weights<MB>(s, sz, sum, w, r16, kap, minus_one);
+        bt_scales(sz, sg.v_sz, n0_next, g);
         bt_lds_order();
-        bt_output<BITS, MB>(val, w, sum, con.lut_v, my.v_shift, patch, lane);
-        val.codes(v_plane, v_half, n0_next, my);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            uint32_t f[4];
+            vc[hf].align(f, my.v_shift);
+#pragma unroll
+            for (int sub = 0; sub < 4; ++sub)
+                bt_products<MB>(bt_value_operand<BITS>(f, sub, con.lut_v), *(const half8_t *)(patch + ((hf * 4 + sub) * 64 + lane) * 16), w, sum, hf * 4 + sub);
+        }
+        vc[0].load(v_plane, n0_next, my);
+        vc[1].load(v_plane + v_half, n0_next, my);
         bt_lds_order();
         if (at.v0 + lane < at.v1) *(uint16_t *)(patch + vp) = 0;
         for (uint32_t e = at.v0 + 64 + lane; e < at.v1; e += 64) *(uint16_t *)(patch + bt_value_place(v_list[e])) = 0;
@@ -745,8 +820,8 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
         at = at_next;
     }
 
-    // ---- the wavefronts' sums to one
-    __syncthreads();
+    // ---- the wavefronts' sums to one: each leaves a block of 16 queries where its patch was (pieces of four channels, in an order that
+    // spreads the queries over the banks), then every thread adds the four
     if (g == 0)
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
@@ -754,34 +829,26 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
             wave_l[wave][mb * 16 + r16] = sum.lz[mb][1];
         }
     __syncthreads();
-    float *sums = (float *)area;
-    float fac[MB];
+    const int64_t slot0 = ((int64_t)p.ch * a.heads + p.h) * a.mp[WHICH] + (int64_t)p.qb * 16 * MB;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int c = mb * 16 + r16;
         const float m = __builtin_fmaxf(__builtin_fmaxf(wave_m[0][c], wave_m[1][c]), __builtin_fmaxf(wave_m[2][c], wave_m[3][c]));
-        fac[mb] = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap);
-    }
-    for (int w = 0; w < BT_WAVES; ++w) {
-        if (wave == w)
+        const float fac = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap), z = __shfl(sum.lz[mb][0], r16);
+        if (mb > 0) __syncthreads();
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                const float z = __shfl(sum.lz[mb][0], r16);
+        for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-                for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float4_t *q = (float4_t *)(sums + (mb * 16 + r16) * OROW + hf * 64 + g * 16 + i * 4);
-                        const float4_t v = bt_channels<MB>(sum, mb, hf, i, z) * fac[mb];
-                        *q = w == 0 ? v : *q + v;
-                    }
-            }
+            for (int i = 0; i < 4; ++i)
+                *(float4_t *)(patch + (r16 * 32 + ((hf * 16 + g * 4 + i) ^ r16)) * 16) = bt_channels<MB>(sum, mb, hf, i, z) * fac;
         __syncthreads();
-    }
-    const int64_t slot0 = ((int64_t)p.ch * a.heads + p.h) * a.mp[WHICH] + (int64_t)p.qb * 16 * MB;
-    for (int i = tid; i < 16 * MB * 32; i += BT_NT) {
-        const int row = i >> 5, c = (i & 31) * 4;
-        if (p.qb * 16 * MB + row < p.n_q) *(float4_t *)(a.w.part_o[WHICH] + (slot0 + row) * 128 + c) = *(const float4_t *)(sums + row * OROW + c);
+        for (int i = tid; i < 16 * 32; i += BT_NT) {
+            const int row = i >> 5, c4 = i & 31;
+            float4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < BT_WAVES; ++w) v += *(const float4_t *)(area + w * BT_PATCH + (row * 32 + (c4 ^ row)) * 16);
+            if (p.qb * 16 * MB + mb * 16 + row < p.n_q) *(float4_t *)(a.w.part_o[WHICH] + (slot0 + mb * 16 + row) * 128 + c4 * 4) = v;
+        }
     }
     if (tid < 16 * MB && p.qb * 16 * MB + tid < p.n_q) {
         float m = KVQ_STAT_FLOOR, l = 0.0f;
@@ -803,8 +870,9 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
     constexpr int MB = 2, TW = BT_WAVES / QW, GROUPS = 2 / TW;        // blocks of 32 tokens that a wavefront multiplies per tile
     constexpr int OROW = 132;
     constexpr int KEYS = 4 * 4 * 2 * 1024;
-    static_assert(TW == 1 || QW * 32 * OROW * 4 <= KEYS + 2 * BT_PATCH, "the sums take the tiles' place");
-    __shared__ __attribute__((aligned(16))) uint8_t keys[KEYS + 2 * BT_PATCH];      // [block of 16][step t][part][lane]; residuals
+    static_assert(TW == 1 || QW * 32 * OROW * 4 <= KEYS + 4 * BT_PATCH, "the sums take the tiles' place");
+    // [block of 16][step t][part][lane] Keys; [block of 32][channel block][lane] residuals; the same of signposts of the Values
+    __shared__ __attribute__((aligned(16))) uint8_t keys[KEYS + 4 * BT_PATCH];
     __shared__ BtConst<BITS> con;
     __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];
     __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
@@ -812,8 +880,8 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4, qg = wave % QW, tg = wave / QW;
     const BtPart p = bt_part<WHICH>(a, 32 * QW);
-    const BtSeg &sg = a.w.segs[p.si];
-    uint8_t *const patches = keys + KEYS;
+    const BtSeg sg = bt_seg(a.w.segs[p.si]);
+    uint8_t *const patches = keys + KEYS, *const values = patches + 2 * BT_PATCH;
 
     con.stage(a, sg, p);
     for (int i = tid; i < 2 * BT_PATCH / 16; i += BT_NT) *(uint4 *)(patches + i * 16) = uint4{0u, 0u, 0u, 0u};
@@ -864,10 +932,11 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
     BtTable tab;
     tab.load(a, place_of(lane));
     BtPlaces at(tab, 0);
-    BtValues<BITS> val;
+    BtCodes<BITS> vc[2];                                         // of both blocks, the half of the channels that has this wavefront's two blocks
     load_keys(0);
-    val.scales(sg.v_sz, block_of(0, tg) * BT_BLOCK, g);
-    val.codes(v_plane, v_half, block_of(0, tg) * BT_BLOCK, my);
+    const uint8_t *const my_half = v_plane + (wave >> 1) * v_half;
+#pragma unroll
+    for (int gr = 0; gr < 2; ++gr) vc[gr].load(my_half, block_of(0, gr) * BT_BLOCK, my);
     if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
     if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
     uint8_t *const my_keys = keys + wave * 8192;
@@ -918,6 +987,23 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
         }
         load_keys(next);
         if (at_next.k0 + lane < at_next.k1) ke = k_list[at_next.k0 + lane];
+        // ---- Values: signposts of two blocks of channels for all 64 tokens; residuals of this wavefront's 16
+        uint32_t sz[GROUPS][2][4];
+#pragma unroll
+        for (int gr = 0; gr < GROUPS; ++gr) bt_scales(sz[gr], sg.v_sz, block_of(tile, TW == 1 ? gr : tg) * BT_BLOCK, g);
+#pragma unroll
+        for (int gr = 0; gr < 2; ++gr) {
+            uint32_t f[4];
+            vc[gr].align(f, my.v_shift);
+            if (wave & 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] >>= 4 * BITS;       // its two blocks are the half's third and fourth
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+                *(half8_t *)(values + ((gr * 8 + 2 * wave + sub) * 64 + lane) * 16) = bt_value_operand<BITS>(f, sub, con.lut_v);
+        }
+#pragma unroll
+        for (int gr = 0; gr < 2; ++gr) vc[gr].load(my_half, block_of(next, gr) * BT_BLOCK, my);
         const uint32_t vp = bt_value_place(ve);
         const bool v_mine = at.v0 + lane < at.v1 && (int)((ve >> 11) & 1u) == half;
         if (v_mine) *(uint16_t *)(my_patch + vp) = (uint16_t)(ve >> 16);
@@ -926,17 +1012,15 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
             if ((int)((x >> 11) & 1u) == half) *(uint16_t *)(my_patch + bt_value_place(x)) = (uint16_t)(x >> 16);
         }
         __syncthreads();
-        // ---- products with this wavefront's queries
+        // ---- products with this wavefront's queries: all scores, their maximum, then weights and output without a branch
+        float4_t s[GROUPS][2][MB];
 #pragma unroll
         for (int gr = 0; gr < GROUPS; ++gr) {
-            const int grp = TW == 1 ? gr : tg, blk = p.b0 + 2 * tile + grp, n0 = blk * BT_BLOCK;
-            const bool edge = n0 < p.first || n0 + BT_BLOCK > p.n || blk >= p.b1;
-            const int blk_next = gr + 1 < GROUPS ? block_of(tile, gr + 1) : block_of(next, TW == 1 ? 0 : tg);
-            float4_t s[2][MB];
+            const int grp = TW == 1 ? gr : tg;
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) s[tb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+                for (int mb = 0; mb < MB; ++mb) s[gr][tb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 half8_t hi[2], lo[2];
@@ -949,21 +1033,33 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) s[tb][mb] = bt_mfma(lo[tb], qf[mb][t][0], s[tb][mb]);
+                    for (int mb = 0; mb < MB; ++mb) s[gr][tb][mb] = bt_mfma(lo[tb], qf[mb][t][0], s[gr][tb][mb]);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) s[tb][mb] = bt_mfma(hi[tb], qf[mb][t][1], s[tb][mb]);
+                    for (int mb = 0; mb < MB; ++mb) s[gr][tb][mb] = bt_mfma(hi[tb], qf[mb][t][1], s[gr][tb][mb]);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) s[tb][mb] = bt_mfma(hi[tb], qf[mb][t][0], s[tb][mb]);
+                    for (int mb = 0; mb < MB; ++mb) s[gr][tb][mb] = bt_mfma(hi[tb], qf[mb][t][0], s[gr][tb][mb]);
             }
+        }
+#pragma unroll
+        for (int gr = 0; gr < GROUPS; ++gr) {
+            const int blk = p.b0 + 2 * tile + (TW == 1 ? gr : tg), n0 = blk * BT_BLOCK;
+            if (n0 < p.first || n0 + BT_BLOCK > p.n || blk >= p.b1) bt_mask<MB>(s[gr], sz[gr], n0, p.first, blk >= p.b1 ? 0 : p.n, g);
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) bt_maximum<MB, GROUPS>(s, sum, mb);
+#pragma unroll
+        for (int gr = 0; gr < GROUPS; ++gr) {
+            const int grp = TW == 1 ? gr : tg;
             BtWeights w[MB];
-            bt_weights<BITS, MB>(s, val, sum, w, edge, n0, p.first, blk >= p.b1 ? 0 : p.n, g, r16, kap, minus_one);
-            val.scales(sg.v_sz, blk_next * BT_BLOCK, g);
-            bt_output<BITS, MB>(val, w, sum, con.lut_v, my.v_shift, patches + grp * BT_PATCH, lane);
-            val.codes(v_plane, v_half, blk_next * BT_BLOCK, my);
+            bt_weights<MB>(s[gr], sz[gr], sum, w, r16, kap, minus_one);
+#pragma unroll
+            for (int cb = 0; cb < 8; ++cb)
+                bt_products<MB>(*(const half8_t *)(values + ((grp * 8 + cb) * 64 + lane) * 16), *(const half8_t *)(patches + ((grp * 8 + cb) * 64 + lane) * 16),
+                                w, sum, cb);
         }
         __syncthreads();
         if (v_mine) *(uint16_t *)(my_patch + vp) = 0;
@@ -1046,7 +1142,7 @@ __global__ __launch_bounds__(256) void kvq_batch_join(BtArgs a)
     // sink tokens: scores from their fp16 rows
     int n_sink[2];
     for (int k = 0; k < 2; ++k) {
-        const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
+        const BtSeg sg = bt_seg(a.w.segs[k == 0 ? 0 : 1 + b]);
         n_sink[k] = sg.n_sink < sg.n ? sg.n_sink : sg.n;
         for (int j = 0; j < n_sink[k]; ++j)
             if (tid < 64) {
@@ -1080,7 +1176,7 @@ __global__ __launch_bounds__(256) void kvq_batch_join(BtArgs a)
     }
     if (slice == 0)
         for (int k = 0; k < 2; ++k) {
-            const BtSeg &sg = a.w.segs[k == 0 ? 0 : 1 + b];
+            const BtSeg sg = bt_seg(a.w.segs[k == 0 ? 0 : 1 + b]);
             for (int j = 0; j < n_sink[k]; ++j) {
                 const float f = __builtin_amdgcn_exp2f(sink_x[k * KVQ_MAX_SINK + j] - m);
                 const uint16_t *row = sg.sink_v + (int64_t)j * a.heads * 128 + h * 128 + c4;
@@ -1121,7 +1217,7 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     memset(&p, 0, sizeof p);
     const kvq_cache *one = prefix;
     if (n_seqs < 1 || n_seqs > (1 << 20)) return KVQ_ERR_INVALID_ARG;
-    int64_t own_blocks = 0, k_entries = 0, v_entries = 0;
+    int64_t own_blocks = 0, own_seqs = 0, k_entries = 0, v_entries = 0;
     auto add = [&](const kvq_cache *c, int64_t &blocks) -> kvq_status {
         const kvq_status st = kvq_check_cache(c);
         if (st != KVQ_OK) return st;
@@ -1145,6 +1241,7 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
         if (caches[b]) {
             const kvq_status st = add(caches[b], own_blocks);
             if (st != KVQ_OK) return st;
+            own_seqs += caches[b]->n_tokens_k > 0;
         }
     if (!one) return KVQ_ERR_INVALID_ARG;
     BtArgs &a = p.a;
@@ -1156,21 +1253,35 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     p.blocks = pre_blocks + own_blocks;
     if (p.blocks * (a.heads + 1) >= ((int64_t)1 << 40) || (int64_t)n_seqs * one->n_q_heads >= ((int64_t)1 << 28)) return KVQ_ERR_UNSUPPORTED;
     const int64_t m[2] = {(int64_t)n_seqs * a.ratio, a.ratio};
-    const int64_t blocks[2] = {pre_blocks, own_blocks};
+    const int64_t blocks[2] = {pre_blocks, own_blocks}, used[2] = {1, own_seqs};
+    int64_t n_chunks[2];
     for (int k = 0; k < 2; ++k) {
         p.mb[k] = bt_mb(m[k]);
         a.mp[k] = (int32_t)((m[k] + 16 * p.mb[k] - 1) / (16 * p.mb[k]) * (16 * p.mb[k]));
-        // as many workgroups as the chip holds at once (or a little under), none with less than a block per wavefront
-        const int64_t per_head = (int64_t)kvq_cu_count() * (p.mb[k] == 1 ? 3 : 2) / ((int64_t)a.heads * (a.mp[k] / (16 * p.mb[k])));
-        int64_t chunk = per_head > 0 ? (blocks[k] + per_head - 1) / per_head : blocks[k];
-        chunk = (chunk + BT_WAVES - 1) / BT_WAVES * BT_WAVES;
-        if (chunk < BT_WAVES) chunk = BT_WAVES;
+        // Workgroups: as many as the chip holds at once, so that none waits for a second round, and none with less than a block per
+        // wavefront.  Sequences are not cut together, so the blocks per workgroup grow until their pieces fit as well (48 of up to
+        // 9000 tokens: 952 workgroups where 768 fit at once took 183 us).
+        const int64_t slots = (int64_t)kvq_cu_count() * (p.mb[k] == 1 ? 3 : 2) / ((int64_t)a.heads * (a.mp[k] / (16 * p.mb[k])));
+        int64_t chunk = slots > 0 ? (blocks[k] + slots - 1) / slots : blocks[k];
+        chunk = chunk < BT_WAVES ? BT_WAVES : (chunk + BT_WAVES - 1) / BT_WAVES * BT_WAVES;
+        auto pieces = [&](int64_t c) {
+            if (k == 0) return (pre_blocks + c - 1) / c;
+            int64_t sum = 0;
+            for (int32_t b = 0; caches && b < n_seqs; ++b)
+                if (caches[b]) sum += ((caches[b]->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK + c - 1) / c;
+            return sum;
+        };
+        int64_t n = pieces(chunk);
+        for (int64_t more = chunk; n > slots && used[k] < slots && more < 2 * chunk;) {
+            more += (more / 16 / BT_WAVES + 1) * BT_WAVES;
+            n = pieces(more);
+            if (n <= slots) chunk = more;
+        }
         a.chunk[k] = (int32_t)chunk;
+        n_chunks[k] = pieces(chunk);
     }
-    a.n_chunks[0] = (int32_t)((pre_blocks + a.chunk[0] - 1) / a.chunk[0]);
-    int64_t own_chunks = 0;
-    for (int32_t b = 0; caches && b < n_seqs; ++b)
-        if (caches[b]) own_chunks += ((caches[b]->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK + a.chunk[1] - 1) / a.chunk[1];
+    a.n_chunks[0] = (int32_t)n_chunks[0];
+    const int64_t own_chunks = n_chunks[1];
     if (own_chunks >= (1 << 24)) return KVQ_ERR_UNSUPPORTED;
     a.n_chunks[1] = (int32_t)own_chunks;
     int64_t at = 0;
@@ -1184,6 +1295,7 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     w.k_start = (uint32_t *)take(4 * p.blocks * (a.heads + 1));
     w.v_start = (uint32_t *)take(4 * p.blocks * (a.heads + 1));
     w.smax = (float *)take(4 * p.blocks);
+    w.owner = (int32_t *)take(4 * own_chunks);
     const int64_t rows = (int64_t)n_seqs * one->n_q_heads;
     for (int k = 0; k < 2; ++k) {
         const int64_t here = blocks[k] > 0 ? rows : 0;
@@ -1250,23 +1362,8 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
 
     // ---- descriptors, BT_SEGS at a time in the arguments of the first kernel
     BtSegs part;
-    int64_t k_list = 0, v_list = 0, blk = 0, chunk = 0;
-    int wgs = 0;
+    int64_t k_list = 0, v_list = 0, blk = 0, chunk = 0, wgs = 0;
     memset(&part, 0, sizeof part);
-    bool rows_done = false;
-    auto flush = [&]() -> kvq_status {
-        part.wg0[part.n] = wgs;
-        // an empty sequence's descriptor has the constants too (rows read the rotary ones)
-        const int64_t rows = (int64_t)n_seqs * one->n_q_heads;
-        const int row_wgs = rows_done ? 0 : (int)((rows + BT_WAVES - 1) / BT_WAVES);
-        rows_done = true;
-        kvq_batch_prepare<<<dim3((unsigned)(row_wgs + wgs > 0 ? row_wgs + 2 * wgs : 1)), dim3(BT_NT), 0, s>>>(a, part, row_wgs);
-        KVQ_HIP_CHECK(hipGetLastError());
-        part.first += part.n;
-        part.n = 0;
-        wgs = 0;
-        return KVQ_OK;
-    };
     for (int32_t i = 0; i <= n_seqs; ++i) {
         const kvq_cache *c = i == 0 ? prefix : caches ? caches[i - 1] : nullptr;
         BtSeg &g = part.seg[part.n];
@@ -1274,9 +1371,9 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
         g.params = one->params;
         g.blk0 = (int32_t)blk;
         g.chunk0 = (int32_t)chunk;
+        g.wg0 = (int32_t)wgs;
         g.k_list = k_list;
         g.v_list = v_list;
-        part.wg0[part.n] = wgs;
         if (c && c->n_tokens_k > 0) {
             g.k_codes = c->k_codes;
             g.v_codes = c->v_codes;
@@ -1302,14 +1399,23 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
             v_list += vr;
             const int64_t nb = (c->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK;
             blk += nb;
-            wgs += (int)nb;
+            wgs += (nb + BT_SORT - 1) / BT_SORT;
             if (i > 0) chunk += (nb + a.chunk[1] - 1) / a.chunk[1];
         }
-        if (++part.n == BT_SEGS || i == n_seqs) {
-            st = flush();
-            if (st != KVQ_OK) return st;
+        if (++part.n < BT_SEGS && i < n_seqs) continue;
+        if (n_seqs + 1 > BT_SEGS) {
+            kvq_batch_upload<<<dim3(1), dim3(BT_NT), 0, s>>>(a, part);
+            KVQ_HIP_CHECK(hipGetLastError());
+        }
+        if (i < n_seqs) {
+            part.first += part.n;
+            part.n = 0;
         }
     }
+    const int64_t row_wgs = ((int64_t)n_seqs * one->n_q_heads + BT_WAVES - 1) / BT_WAVES;
+    if (row_wgs + 2 * wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
+    kvq_batch_prepare<<<dim3((unsigned)(row_wgs + 2 * wgs)), dim3(BT_NT), 0, s>>>(a, part, (int)row_wgs, n_seqs + 1);
+    KVQ_HIP_CHECK(hipGetLastError());
     st = bt_launch<0>(a, one->bits, p.mb[0], s);
     if (st == KVQ_OK) st = bt_launch<1>(a, one->bits, p.mb[1], s);
     if (st != KVQ_OK) return st;

@@ -134,15 +134,19 @@ __device__ void mv_values(const MvJob &j, const int32_t *tokens, int item, int l
     for (int p = 0; p < BITS; ++p) *(uint4 *)(o + p * 1024) = uint4{c[4 * p], c[4 * p + 1], c[4 * p + 2], c[4 * p + 3]};
 }
 
+// (A block's address comes out of memory: the cast says that it points to global memory.)
+__device__ __forceinline__ uint16_t *mv_block(const void *arr, uint32_t b)
+{
+    return (uint16_t *)(__attribute__((address_space(1))) uint16_t *)(uintptr_t)((uint16_t *const *)arr)[b];
+}
 __device__ __forceinline__ uint16_t mv_get(const void *arr, int shift, uint32_t e)
 {
-    if (shift == 0) return ((const uint16_t *)arr)[e];
-    return ((const uint16_t *const *)arr)[e >> shift][e & ((1u << shift) - 1u)];
+    return shift == 0 ? ((const uint16_t *)arr)[e] : mv_block(arr, e >> shift)[e & ((1u << shift) - 1u)];
 }
 __device__ __forceinline__ void mv_put(void *arr, int shift, uint32_t e, uint16_t x)
 {
     if (shift == 0) ((uint16_t *)arr)[e] = x;
-    else ((uint16_t *const *)arr)[e >> shift][e & ((1u << shift) - 1u)] = x;
+    else mv_block(arr, e >> shift)[e & ((1u << shift) - 1u)] = x;
 }
 
 // n consecutive 16-bit entries from place s to place d, by the whole workgroup: where both ends are flat arrays in pieces of 16
