@@ -111,23 +111,23 @@ __device__ __forceinline__ uint32_t bt_entry(const void *arr, int shift, uint32_
     return bt_global(((const uint16_t *const *)arr)[e >> shift])[e & ((1u << shift) - 1u)];
 }
 
-// The entries of four blocks of 32 tokens sorted by block and head: eight lanes a token, an entry's rank among its head's from the count
+// The entries of two blocks of 32 tokens sorted by block and head: eight lanes a token, an entry's rank among its head's from the count
 // that it adds to, its place from the sums of the counts.  (The order within a head is any: every entry has an element of its own.)
 // A lane keeps up to BT_HELD entries of each block in registers from the count to the placing; where a token has more (over 48)
-// they are read twice.  Each stage is a round trip to memory, so the four blocks go through them together (one block per
-// workgroup: 46 us over 48 sequences of 9000 tokens, 29 with four).  The sorted entries leave through LDS: stored straight to their
-// places, a line each, they take 45 us over 131072 tokens of 32 heads (ONEUS so).
-constexpr int BT_HELD = 6, BT_SORT = 4, BT_STAGE = BT_SORT * BT_BLOCK * 8 * BT_HELD;
+// they are read twice.  Each stage is a round trip to memory or to LDS, and how many blocks a compute unit has under way decides:
+// 131072 tokens of 32 heads take 40 us with one block per workgroup, 31 with two, 35 with four; to LDS first and from there in
+// order to memory 32; 64 tokens' entries dealt out evenly, with a search for each lane's token, 69.
+constexpr int BT_HELD = 6, BT_SORT = 2;
 
 template <bool BLOCKED>
 __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int n,
-                             int heads, uint32_t *start, uint32_t *list, uint32_t *count, uint32_t *stage)
+                             int heads, uint32_t *start, uint32_t *list, uint32_t *count)
 {
     const int tid = threadIdx.x, t = tid >> 3, l = tid & 7, lane = tid & 63, wave = tid >> 6;
     for (int h = tid; h < BT_SORT * heads; h += BT_NT) count[h] = 0u;
-    uint32_t p0[BT_SORT], p1[BT_SORT], x[BT_SORT][BT_HELD], rank[BT_SORT][BT_HELD];
+    uint32_t p0[BT_SORT], p1[BT_SORT], x[BT_SORT][BT_HELD], v[BT_SORT][BT_HELD], rank[BT_SORT][BT_HELD];
     const int my_first = n0 + wave * BT_BLOCK;                   // first token of the block whose sums this wavefront takes
-    const uint32_t base = my_first < n ? ptr[my_first] : 0u, all0 = ptr[n0];
+    const uint32_t base = my_first < n ? ptr[my_first] : 0u;
 #pragma unroll
     for (int b = 0; b < BT_SORT; ++b) {
         const int m = n0 + b * BT_BLOCK + t;
@@ -142,9 +142,19 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
 #pragma unroll
         for (int i = 0; i < BT_HELD; ++i) {
             const uint32_t e = p0[b] + l + 8 * i;
-            if (e < p1[b]) x[b][i] = bt_entry<BLOCKED>(idx, shift, e) | (bt_entry<BLOCKED>(val, shift, e) << 16);
+            if (e < p1[b]) {
+                x[b][i] = bt_entry<BLOCKED>(idx, shift, e);
+                v[b][i] = bt_entry<BLOCKED>(val, shift, e);      // (put together below, behind the asm: in here each pair would be waited for by itself)
+            }
         }
     }
+#pragma unroll
+    for (int b = 0; b < BT_SORT; ++b)
+#pragma unroll
+        for (int i = 0; i < BT_HELD; ++i) {
+            asm volatile("" : "+v"(v[b][i]));
+            x[b][i] |= v[b][i] << 16;
+        }
     const bool many = __syncthreads_or(more) != 0;
 #pragma unroll
     for (int b = 0; b < BT_SORT; ++b) {
@@ -161,8 +171,7 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
         }
     }
     __syncthreads();
-    {                                               // exclusive sums, a wavefront a block, up to eight heads a lane
-        static_assert(BT_SORT == BT_WAVES, "a wavefront per block");
+    if (wave < BT_SORT) {                           // exclusive sums, a wavefront a block, up to eight heads a lane
         uint32_t c[BT_MAX_HEADS / 64], s = 0, *const mine = count + wave * heads;
         const int per = (heads + 63) / 64;
 #pragma unroll
@@ -199,8 +208,8 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
             for (int i = 0; i < BT_HELD; ++i) {
                 const uint32_t c = x[b][i] & 0xFFFFu;
                 if (p0[b] + l + 8 * i < p1[b] && (c >> 7) < (uint32_t)heads) {
-                    const uint32_t at = mine[c >> 7] + rank[b][i] - all0;
-                    if (at < (uint32_t)BT_STAGE) stage[at] = (x[b][i] & 0xFFFF0000u) | ((uint32_t)t << 7) | (c & 127u);
+                    const uint32_t at = mine[c >> 7] + rank[b][i];
+                    if (at < room) list[at] = (x[b][i] & 0xFFFF0000u) | ((uint32_t)t << 7) | (c & 127u);
                 }
             }
         } else {
@@ -212,11 +221,6 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
                 }
             }
         }
-    }
-    if (!many) {
-        __syncthreads();
-        const uint32_t all = ptr[n0 + BT_SORT * BT_BLOCK < n ? n0 + BT_SORT * BT_BLOCK : n], end = all < room ? all : room;
-        for (uint32_t i = tid; all0 + i < end; i += BT_NT) list[all0 + i] = stage[i];
     }
 }
 
@@ -264,7 +268,7 @@ __global__ __launch_bounds__(BT_NT) void kvq_batch_upload(BtArgs a, BtSegs s) { 
 // arguments brings them along; otherwise (`total` > s.n) they are in memory already.
 __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, int row_wgs, int total)
 {
-    __shared__ uint32_t count[BT_SORT * BT_MAX_HEADS], stage[BT_STAGE];
+    __shared__ uint32_t count[BT_SORT * BT_MAX_HEADS];
     const int tid = threadIdx.x, lane = tid & 63;
     int wg = blockIdx.x;
     if (wg == 0 && total == s.n) bt_upload(a, s);
@@ -300,8 +304,8 @@ __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, i
     if (blk == 0 && values && i > 0)                // the workgroups of a sequence's own tokens find it by their number
         for (int c = tid; c < (g.n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK); c += BT_NT) a.w.owner[g.chunk0 + c] = i;
     uint32_t *start = (values ? a.w.v_start : a.w.k_start) + at, *list = values ? a.w.v_list + g.v_list : a.w.k_list + g.k_list;
-    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n, a.heads, start, list, count, stage);
-    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n, a.heads, start, list, count, stage);
+    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n, a.heads, start, list, count);
+    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n, a.heads, start, list, count);
     if (values && tid < BT_SORT * BT_BLOCK) {
         float m = 0.0f;
         if (n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
