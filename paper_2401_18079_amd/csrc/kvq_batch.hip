@@ -25,6 +25,7 @@
 // scatters its head's residuals into a zeroed patch that it reads beside the codes.
 #include <math.h>
 #include <string.h>
+#include <type_traits>
 #include "kvq_common.hpp"
 #include "kvq_qk_sparse.hpp"
 
@@ -374,14 +375,14 @@ struct BtPart {
 };
 
 template <int WHICH>
-__device__ __forceinline__ BtPart bt_part(const BtArgs &a, int queries)
+__device__ __forceinline__ BtPart bt_part(const BtArgs &a, int wg, int queries)
 {
     BtPart p;
-    // grid: query blocks innermost (they read the same codes), then heads, then chunks
+    // workgroups: query blocks innermost (they read the same codes), then heads, then chunks
     const int qblocks = a.mp[WHICH] / queries;
-    p.qb = blockIdx.x % qblocks;
-    p.h = (blockIdx.x / qblocks) % a.heads;
-    p.ch = blockIdx.x / (qblocks * a.heads);
+    p.qb = wg % qblocks;
+    p.h = (wg / qblocks) % a.heads;
+    p.ch = wg / (qblocks * a.heads);
     p.si = WHICH == 1 ? a.w.owner[p.ch] : 0;
     const BtSeg &sg = a.w.segs[p.si];
     p.n = sg.n;
@@ -663,20 +664,31 @@ struct BtPlaces {
 // wavefronts every fourth block from the codes to the output.  WHICH = 0: the prefix, every sequence's queries; 1: a sequence's
 // own tokens, its own queries.
 template <int BITS, int MB, int WHICH>
-__global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArgs a)
-{
-    constexpr int QBYTES = 8192 * MB;
-    constexpr int PATCHES = BT_WAVES * BT_PATCH;
+struct BtAlone {
+    static constexpr int PER_CU = MB == 1 ? 3 : 2;
+    static constexpr int QBYTES = 8192 * MB, PATCHES = BT_WAVES * BT_PATCH;
     static_assert(16 * 128 * 4 == BT_PATCH, "the sums of 16 queries take a patch's place");
-    __shared__ __attribute__((aligned(16))) uint8_t area[PATCHES];
-    __shared__ __attribute__((aligned(16))) uint8_t qfrag[QBYTES];
-    __shared__ BtConst<BITS> con;
-    __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];               // angles at a block's first token
-    __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
+    struct Shared {
+        __attribute__((aligned(16))) uint8_t area[PATCHES], qfrag[QBYTES];
+        __attribute__((aligned(16))) float base[BT_WAVES][64];                      // angles at a block's first token
+        BtConst<BITS> con;
+        float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
+    };
+    static __device__ void run(const BtArgs &a, int wg, Shared &sh);
+};
 
+template <int BITS, int MB, int WHICH>
+__device__ __forceinline__ void BtAlone<BITS, MB, WHICH>::run(const BtArgs &a, int wg, Shared &sh)
+{
+    auto &area = sh.area;
+    auto &qfrag = sh.qfrag;
+    auto &con = sh.con;
+    auto &base = sh.base;
+    auto &wave_m = sh.wave_m;
+    auto &wave_l = sh.wave_l;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4;
-    const BtPart p = bt_part<WHICH>(a, 16 * MB);
+    const BtPart p = bt_part<WHICH>(a, wg, 16 * MB);
     const BtSeg sg = bt_seg(a.w.segs[p.si]);
 
     uint8_t *const patch = area + wave * BT_PATCH;
@@ -869,21 +881,32 @@ __global__ __launch_bounds__(BT_NT, MB == 1 ? 3 : 2) void kvq_batch_attend(BtArg
 // The Keys' residuals are added where the rotated pairs lie, by a lane per entry: entries of channels below 64 first, so that two of
 // one pair never meet.
 template <int BITS, int QW, int WHICH>
-__global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
-{
-    constexpr int MB = 2, TW = BT_WAVES / QW, GROUPS = 2 / TW;        // blocks of 32 tokens that a wavefront multiplies per tile
-    constexpr int OROW = 132;
-    constexpr int KEYS = 4 * 4 * 2 * 1024;
+struct BtTogether {
+    static constexpr int PER_CU = 2;
+    static constexpr int MB = 2, TW = BT_WAVES / QW, GROUPS = 2 / TW;       // blocks of 32 tokens that a wavefront multiplies per tile
+    static constexpr int OROW = 132, KEYS = 4 * 4 * 2 * 1024;
     static_assert(TW == 1 || QW * 32 * OROW * 4 <= KEYS + 4 * BT_PATCH, "the sums take the tiles' place");
-    // [block of 16][step t][part][lane] Keys; [block of 32][channel block][lane] residuals; the same of signposts of the Values
-    __shared__ __attribute__((aligned(16))) uint8_t keys[KEYS + 4 * BT_PATCH];
-    __shared__ BtConst<BITS> con;
-    __shared__ __attribute__((aligned(16))) float base[BT_WAVES][64];
-    __shared__ float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
+    struct Shared {
+        // [block of 16][step t][part][lane] Keys; [block of 32][channel block][lane] residuals; the same of signposts of the Values
+        __attribute__((aligned(16))) uint8_t keys[KEYS + 4 * BT_PATCH];
+        __attribute__((aligned(16))) float base[BT_WAVES][64];
+        BtConst<BITS> con;
+        float wave_m[BT_WAVES][16 * MB], wave_l[BT_WAVES][16 * MB];
+    };
+    static __device__ void run(const BtArgs &a, int wg, Shared &sh);
+};
 
+template <int BITS, int QW, int WHICH>
+__device__ __forceinline__ void BtTogether<BITS, QW, WHICH>::run(const BtArgs &a, int wg, Shared &sh)
+{
+    auto &keys = sh.keys;
+    auto &con = sh.con;
+    auto &base = sh.base;
+    auto &wave_m = sh.wave_m;
+    auto &wave_l = sh.wave_l;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4, qg = wave % QW, tg = wave / QW;
-    const BtPart p = bt_part<WHICH>(a, 32 * QW);
+    const BtPart p = bt_part<WHICH>(a, wg, 32 * QW);
     const BtSeg sg = bt_seg(a.w.segs[p.si]);
     uint8_t *const patches = keys + KEYS, *const values = patches + 2 * BT_PATCH;
 
@@ -1006,8 +1029,10 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
             for (int sub = 0; sub < 2; ++sub)
                 *(half8_t *)(values + ((gr * 8 + 2 * wave + sub) * 64 + lane) * 16) = bt_value_operand<BITS>(f, sub, con.lut_v);
         }
+        // (requested ahead of the products where there are registers for it: with 128 queries there are not)
+        if (TW == 2)
 #pragma unroll
-        for (int gr = 0; gr < 2; ++gr) vc[gr].load(my_half, block_of(next, gr) * BT_BLOCK, my);
+            for (int gr = 0; gr < 2; ++gr) vc[gr].load(my_half, block_of(next, gr) * BT_BLOCK, my);
         const uint32_t vp = bt_value_place(ve);
         const bool v_mine = at.v0 + lane < at.v1 && (int)((ve >> 11) & 1u) == half;
         if (v_mine) *(uint16_t *)(my_patch + vp) = (uint16_t)(ve >> 16);
@@ -1065,6 +1090,9 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
                 bt_products<MB>(*(const half8_t *)(values + ((grp * 8 + cb) * 64 + lane) * 16), *(const half8_t *)(patches + ((grp * 8 + cb) * 64 + lane) * 16),
                                 w, sum, cb);
         }
+        if (TW == 1)
+#pragma unroll
+            for (int gr = 0; gr < 2; ++gr) vc[gr].load(my_half, block_of(next, gr) * BT_BLOCK, my);
         __syncthreads();
         if (v_mine) *(uint16_t *)(my_patch + vp) = 0;
         for (uint32_t e = at.v0 + 64 + lane; e < at.v1; e += 64) {
@@ -1122,6 +1150,31 @@ __global__ __launch_bounds__(BT_NT, 2) void kvq_batch_team(BtArgs a)
         }
         if (TW == 2) __syncthreads();
     }
+}
+
+// The launch: the prefix's workgroups (queries in blocks of 16 MBP), then those of the sequences' own tokens (MBO); 0: none of the kind.
+struct BtNone {
+    static constexpr int PER_CU = 3;
+    struct Shared {
+        int none;
+    };
+    static __device__ __forceinline__ void run(const BtArgs &, int, Shared &) {}
+};
+template <int BITS, int MB, int WHICH>
+struct BtFormOf {
+    typedef std::conditional_t<(MB <= 2), BtAlone<BITS, (MB == 2 ? 2 : 1), WHICH>, BtTogether<BITS, (MB >= 4 ? MB / 2 : 2), WHICH>> some;
+    typedef std::conditional_t<MB == 0, BtNone, some> type;
+};
+constexpr int bt_per_cu(int mbp, int mbo) { return mbp <= 1 && mbo <= 1 ? 3 : 2; }
+
+template <int BITS, int MBP, int MBO>
+__global__ __launch_bounds__(BT_NT, bt_per_cu(MBP, MBO)) void kvq_batch_attend(BtArgs a, int prefix_wgs)
+{
+    typedef typename BtFormOf<BITS, MBP, 0>::type P;
+    typedef typename BtFormOf<BITS, MBO, 1>::type O;
+    __shared__ __attribute__((aligned(16))) uint8_t mem[sizeof(typename P::Shared) > sizeof(typename O::Shared) ? sizeof(typename P::Shared) : sizeof(typename O::Shared)];
+    if (MBO == 0 || (MBP > 0 && (int)blockIdx.x < prefix_wgs)) P::run(a, blockIdx.x, *(typename P::Shared *)mem);
+    else O::run(a, (int)blockIdx.x - prefix_wgs, *(typename O::Shared *)mem);
 }
 
 // Third kernel: a workgroup per (sequence, query head) joins the workgroups' sums and the attention-sink tokens.  Eight slices of
@@ -1212,8 +1265,10 @@ struct BtPlan {
 
 int64_t bt_up(int64_t n) { return (n + 255) & ~(int64_t)255; }
 
-// Blocks of 16 queries that a workgroup takes: one or two, each of its wavefronts alone; four or eight, together.
-int bt_mb(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : queries <= 64 ? 4 : 8; }
+// Blocks of 16 queries that a workgroup takes: one or two, each of its wavefronts alone; four or eight, together.  (A sequence's own
+// queries rarely fill more than one: two and eight have no form of their own there.)
+int bt_mb_prefix(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : queries <= 64 ? 4 : 8; }
+int bt_mb_own(int64_t queries) { return queries <= 16 ? 1 : 4; }
 
 // The tokens of a call and the places of everything in the workspace (from `base`, which may be null).
 kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int32_t n_seqs, char *base, BtPlan &p)
@@ -1258,35 +1313,60 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     if (p.blocks * (a.heads + 1) >= ((int64_t)1 << 40) || (int64_t)n_seqs * one->n_q_heads >= ((int64_t)1 << 28)) return KVQ_ERR_UNSUPPORTED;
     const int64_t m[2] = {(int64_t)n_seqs * a.ratio, a.ratio};
     const int64_t blocks[2] = {pre_blocks, own_blocks}, used[2] = {1, own_seqs};
-    int64_t n_chunks[2];
     for (int k = 0; k < 2; ++k) {
-        p.mb[k] = bt_mb(m[k]);
-        a.mp[k] = (int32_t)((m[k] + 16 * p.mb[k] - 1) / (16 * p.mb[k]) * (16 * p.mb[k]));
-        // Workgroups: as many as the chip holds at once, so that none waits for a second round, and none with less than a block per
-        // wavefront.  Sequences are not cut together, so the blocks per workgroup grow until their pieces fit as well (48 of up to
-        // 9000 tokens: 952 workgroups where 768 fit at once took 183 us).
-        const int64_t slots = (int64_t)kvq_cu_count() * (p.mb[k] == 1 ? 3 : 2) / ((int64_t)a.heads * (a.mp[k] / (16 * p.mb[k])));
+        p.mb[k] = blocks[k] == 0 ? 0 : k == 0 ? bt_mb_prefix(m[k]) : bt_mb_own(m[k]);
+        const int q = 16 * (p.mb[k] ? p.mb[k] : 1);
+        a.mp[k] = (int32_t)((m[k] + q - 1) / q * q);
+    }
+    // Workgroups: as many as the chip holds at once, so that none waits for a second round, and none with less than a block per
+    // wavefront.  Sequences are not cut together, so the blocks per workgroup grow until their pieces fit as well (48 sequences
+    // of up to 9000 tokens: 952 workgroups where 768 fit at once took 183 us).  Behind a prefix the sequences' own workgroups are
+    // many and short: they are cut fine and get the places that their work, start included, would keep busy meanwhile.
+    auto pieces = [&](int k, int64_t c) {
+        if (k == 0) return (pre_blocks + c - 1) / c;
+        int64_t sum = 0;
+        for (int32_t b = 0; caches && b < n_seqs; ++b)
+            if (caches[b]) sum += ((caches[b]->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK + c - 1) / c;
+        return sum;
+    };
+    auto fit = [&](int k, int64_t slots) {                   // blocks per workgroup for so many workgroups per head and query block
         int64_t chunk = slots > 0 ? (blocks[k] + slots - 1) / slots : blocks[k];
         chunk = chunk < BT_WAVES ? BT_WAVES : (chunk + BT_WAVES - 1) / BT_WAVES * BT_WAVES;
-        auto pieces = [&](int64_t c) {
-            if (k == 0) return (pre_blocks + c - 1) / c;
-            int64_t sum = 0;
-            for (int32_t b = 0; caches && b < n_seqs; ++b)
-                if (caches[b]) sum += ((caches[b]->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK + c - 1) / c;
-            return sum;
-        };
-        int64_t n = pieces(chunk);
-        for (int64_t more = chunk; n > slots && used[k] < slots && more < 2 * chunk;) {
-            more += (more / 16 / BT_WAVES + 1) * BT_WAVES;
-            n = pieces(more);
-            if (n <= slots) chunk = more;
+        if (k == 0 || used[k] >= slots) return chunk;
+        for (int64_t c = chunk; c < 2 * chunk; c += (c / 16 / BT_WAVES + 1) * BT_WAVES)
+            if (pieces(k, c) <= slots) return c;
+        return chunk;
+    };
+    const int64_t places = (int64_t)kvq_cu_count() * bt_per_cu(p.mb[0], p.mb[1]);
+    const int64_t wide[2] = {(int64_t)a.heads * (a.mp[0] / (16 * (p.mb[0] ? p.mb[0] : 1))), (int64_t)a.heads * (a.mp[1] / (16 * (p.mb[1] ? p.mb[1] : 1)))};
+    int64_t own_places = p.mb[0] ? 0 : places;
+    a.chunk[0] = a.chunk[1] = BT_WAVES;
+    if (p.mb[0] == 8 && p.mb[1]) {                           // two launches (bt_launch_bits)
+        a.chunk[0] = (int32_t)fit(0, (int64_t)kvq_cu_count() * bt_per_cu(8, 0) / wide[0]);
+        a.chunk[1] = (int32_t)fit(1, (int64_t)kvq_cu_count() * bt_per_cu(0, p.mb[1]) / wide[1]);
+    } else if (p.mb[0] && p.mb[1]) {
+        // in steps of a block and wavefront: a workgroup's start and end are worth three, a block for 64 or 128 queries three
+        const int64_t cost = p.mb[0] == 4 ? 3 : 1;
+        for (int i = 0; i < 4; ++i) {
+            int64_t left = (places - own_places) / wide[0];
+            if (left < 1) left = 1;
+            a.chunk[0] = (int32_t)fit(0, left);
+            a.chunk[1] = (int32_t)fit(1, own_places > 0 ? 2 * own_places / wide[1] + 1 : 1);
+            const int64_t last = a.chunk[0] / BT_WAVES * cost + 3, each = a.chunk[1] / BT_WAVES + 3;
+            if (each > last / 2 + 3) a.chunk[1] = (int32_t)((last / 2 > 1 ? last / 2 : 1) * BT_WAVES);
+            own_places = (pieces(1, a.chunk[1]) * wide[1] * (a.chunk[1] / BT_WAVES + 3) + last - 1) / last;
+            if (own_places > places / 2) own_places = places / 2;
         }
-        a.chunk[k] = (int32_t)chunk;
-        n_chunks[k] = pieces(chunk);
+        a.chunk[0] = (int32_t)fit(0, (places - own_places) / wide[0] > 0 ? (places - own_places) / wide[0] : 1);
+    } else if (p.mb[0]) {
+        a.chunk[0] = (int32_t)fit(0, places / wide[0]);
+    } else if (p.mb[1]) {
+        a.chunk[1] = (int32_t)fit(1, places / wide[1]);
     }
+    const int64_t n_chunks[2] = {pieces(0, a.chunk[0]), pieces(1, a.chunk[1])};
     a.n_chunks[0] = (int32_t)n_chunks[0];
     const int64_t own_chunks = n_chunks[1];
-    if (own_chunks >= (1 << 24)) return KVQ_ERR_UNSUPPORTED;
+    if (own_chunks >= (1 << 24) || n_chunks[0] * wide[0] + own_chunks * wide[1] >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
     a.n_chunks[1] = (int32_t)own_chunks;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -1315,27 +1395,43 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     return KVQ_OK;
 }
 
-template <int BITS, int WHICH>
-kvq_status bt_launch_bits(const BtArgs &a, int mb, hipStream_t s)
+template <int BITS, int MBP>
+kvq_status bt_launch_own(const BtArgs &a, int mbo, int64_t prefix_wgs, int64_t wgs, hipStream_t s)
 {
-    const int64_t wgs = (int64_t)a.n_chunks[WHICH] * a.heads * (a.mp[WHICH] / (16 * mb));
-    if (wgs == 0) return KVQ_OK;
-    if (wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)wgs), block(BT_NT);
-    if (mb == 1) kvq_batch_attend<BITS, 1, WHICH><<<grid, block, 0, s>>>(a);
-    else if (mb == 2) kvq_batch_attend<BITS, 2, WHICH><<<grid, block, 0, s>>>(a);
-    else if (mb == 4) kvq_batch_team<BITS, 2, WHICH><<<grid, block, 0, s>>>(a);
-    else kvq_batch_team<BITS, 4, WHICH><<<grid, block, 0, s>>>(a);
+    if constexpr (MBP == 8) kvq_batch_attend<BITS, 8, 0><<<grid, block, 0, s>>>(a, (int)prefix_wgs);
+    else if (mbo == 1) kvq_batch_attend<BITS, MBP, 1><<<grid, block, 0, s>>>(a, (int)prefix_wgs);
+    else if (mbo == 4) kvq_batch_attend<BITS, MBP, 4><<<grid, block, 0, s>>>(a, (int)prefix_wgs);
+    else if constexpr (MBP > 0) kvq_batch_attend<BITS, MBP, 0><<<grid, block, 0, s>>>(a, (int)prefix_wgs);
     KVQ_HIP_CHECK(hipGetLastError());
     return KVQ_OK;
 }
 
-template <int WHICH>
-kvq_status bt_launch(const BtArgs &a, int bits, int mb, hipStream_t s)
+template <int BITS>
+kvq_status bt_launch_bits(const BtPlan &p, hipStream_t s)
 {
-    if (bits == 2) return bt_launch_bits<2, WHICH>(a, mb, s);
-    if (bits == 3) return bt_launch_bits<3, WHICH>(a, mb, s);
-    return bt_launch_bits<4, WHICH>(a, mb, s);
+    const BtArgs &a = p.a;
+    int64_t wgs[2];
+    for (int k = 0; k < 2; ++k) wgs[k] = p.mb[k] ? (int64_t)a.n_chunks[k] * a.heads * (a.mp[k] / (16 * p.mb[k])) : 0;
+    const int64_t all = wgs[0] + wgs[1];
+    if (all == 0) return KVQ_OK;
+    if (p.mb[0] == 8) {
+        // The form for 128 queries has no register to spare: beside another form in one kernel it spills more, and its launches are long
+        // enough to stand alone (32 sequences of 32 heads on 8 behind 524287 tokens: 1212 us in one launch, TWOUS in two).
+        const kvq_status st = bt_launch_own<BITS, 8>(a, 0, wgs[0], wgs[0], s);
+        return st != KVQ_OK || wgs[1] == 0 ? st : bt_launch_own<BITS, 0>(a, p.mb[1], 0, wgs[1], s);
+    }
+    switch (p.mb[0]) {
+    case 0: return bt_launch_own<BITS, 0>(a, p.mb[1], 0, all, s);
+    case 1: return bt_launch_own<BITS, 1>(a, p.mb[1], wgs[0], all, s);
+    case 2: return bt_launch_own<BITS, 2>(a, p.mb[1], wgs[0], all, s);
+    default: return bt_launch_own<BITS, 4>(a, p.mb[1], wgs[0], all, s);
+    }
+}
+
+kvq_status bt_launch(const BtPlan &p, int bits, hipStream_t s)
+{
+    return bits == 2 ? bt_launch_bits<2>(p, s) : bits == 3 ? bt_launch_bits<3>(p, s) : bt_launch_bits<4>(p, s);
 }
 
 }  // namespace
@@ -1420,8 +1516,7 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
     if (row_wgs + 2 * wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
     kvq_batch_prepare<<<dim3((unsigned)(row_wgs + 2 * wgs)), dim3(BT_NT), 0, s>>>(a, part, (int)row_wgs, n_seqs + 1);
     KVQ_HIP_CHECK(hipGetLastError());
-    st = bt_launch<0>(a, one->bits, p.mb[0], s);
-    if (st == KVQ_OK) st = bt_launch<1>(a, one->bits, p.mb[1], s);
+    st = bt_launch(p, one->bits, s);
     if (st != KVQ_OK) return st;
     kvq_batch_join<<<dim3((unsigned)(n_seqs * one->n_q_heads)), dim3(256), 0, s>>>(a);
     KVQ_HIP_CHECK(hipGetLastError());
