@@ -42,6 +42,7 @@ constexpr int BT_SEGS = 24;             // descriptors that travel in one launch
 constexpr int BT_MAX_HEADS = 512;
 constexpr int BT_PATCH = 8192;          // bytes of a wavefront's patch
 constexpr float BT_MAX_SLACK = 6.0f;    // the running maximum follows a larger score from 2^6 times the weight on
+constexpr int64_t BT_OWN_ROUNDS = 3;    // workgroups of a batch without a prefix, in times what the chip holds
 constexpr int BT_KAPPA = 9;             // 2^(6 + 9) is the largest weight then
 
 // One cache as the kernels see it.
@@ -88,8 +89,8 @@ struct BtSegs {
 static_assert(sizeof(BtArgs) + sizeof(BtSegs) + 16 <= 4096, "kernel arguments");
 
 // A pointer that came out of memory, as one to global memory: the compiler takes it for one that may point to LDS as well, and loads
-// through such a pointer are waited for together with the LDS, the requests of the next step among them.  (Eight queries over
-// 131072 tokens, 32 heads: FLATUS us with such loads, GLOBALUS with these.)
+// through such a pointer are waited for together with the LDS, the requests of the next step among them.  (128 queries on each of
+// 8 heads, 524287 tokens: 1132 us with such loads, 1074 with these.)
 template <class T>
 __device__ __forceinline__ T *bt_global(T *p)
 {
@@ -1318,10 +1319,11 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
         const int q = 16 * (p.mb[k] ? p.mb[k] : 1);
         a.mp[k] = (int32_t)((m[k] + q - 1) / q * q);
     }
-    // Workgroups: as many as the chip holds at once, so that none waits for a second round, and none with less than a block per
-    // wavefront.  Sequences are not cut together, so the blocks per workgroup grow until their pieces fit as well (48 sequences
-    // of up to 9000 tokens: 952 workgroups where 768 fit at once took 183 us).  Behind a prefix the sequences' own workgroups are
-    // many and short: they are cut fine and get the places that their work, start included, would keep busy meanwhile.
+    // Workgroups: none with less than a block per wavefront.  A prefix is cut into as many as the chip holds at once.  Sequences are
+    // not cut together and their last pieces are short, so without a prefix there are three times as many, dealt out as places
+    // fall free (8 heads, 48 sequences of up to 9000 tokens: 219 us in one round, 182 in two, 177 in three, 181 in four; 48 of 4500
+    // tokens each: 160, 156, 160, 177).  Behind a prefix the sequences' own workgroups are many and short: they are cut fine and get
+    // the places that their work, start included, would keep busy meanwhile.
     auto pieces = [&](int k, int64_t c) {
         if (k == 0) return (pre_blocks + c - 1) / c;
         int64_t sum = 0;
@@ -1343,7 +1345,7 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     a.chunk[0] = a.chunk[1] = BT_WAVES;
     if (p.mb[0] == 8 && p.mb[1]) {                           // two launches (bt_launch_bits)
         a.chunk[0] = (int32_t)fit(0, (int64_t)kvq_cu_count() * bt_per_cu(8, 0) / wide[0]);
-        a.chunk[1] = (int32_t)fit(1, (int64_t)kvq_cu_count() * bt_per_cu(0, p.mb[1]) / wide[1]);
+        a.chunk[1] = (int32_t)fit(1, BT_OWN_ROUNDS * kvq_cu_count() * bt_per_cu(0, p.mb[1]) / wide[1]);
     } else if (p.mb[0] && p.mb[1]) {
         // in steps of a block and wavefront: a workgroup's start and end are worth three, a block for 64 or 128 queries three
         const int64_t cost = p.mb[0] == 4 ? 3 : 1;
@@ -1361,7 +1363,7 @@ kvq_status bt_plan(const kvq_cache *prefix, const kvq_cache *const *caches, int3
     } else if (p.mb[0]) {
         a.chunk[0] = (int32_t)fit(0, places / wide[0]);
     } else if (p.mb[1]) {
-        a.chunk[1] = (int32_t)fit(1, places / wide[1]);
+        a.chunk[1] = (int32_t)fit(1, BT_OWN_ROUNDS * places / wide[1]);
     }
     const int64_t n_chunks[2] = {pieces(0, a.chunk[0]), pieces(1, a.chunk[1])};
     a.n_chunks[0] = (int32_t)n_chunks[0];
@@ -1417,7 +1419,7 @@ kvq_status bt_launch_bits(const BtPlan &p, hipStream_t s)
     if (all == 0) return KVQ_OK;
     if (p.mb[0] == 8) {
         // The form for 128 queries has no register to spare: beside another form in one kernel it spills more, and its launches are long
-        // enough to stand alone (32 sequences of 32 heads on 8 behind 524287 tokens: 1212 us in one launch, TWOUS in two).
+        // enough to stand alone (32 sequences of 32 heads on 8 behind 524287 tokens: 1212 us in one launch, 1087 in two).
         const kvq_status st = bt_launch_own<BITS, 8>(a, 0, wgs[0], wgs[0], s);
         return st != KVQ_OK || wgs[1] == 0 ? st : bt_launch_own<BITS, 0>(a, p.mb[1], 0, wgs[1], s);
     }
