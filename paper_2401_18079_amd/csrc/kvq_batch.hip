@@ -116,14 +116,15 @@ __device__ __forceinline__ uint32_t bt_entry(const void *arr, int shift, uint32_
 // The entries of two blocks of 32 tokens sorted by block and head: eight lanes a token, an entry's rank among its head's from the count
 // that it adds to, its place from the sums of the counts.  (The order within a head is any: every entry has an element of its own.)
 // A lane keeps up to BT_HELD entries of each block in registers from the count to the placing; where a token has more (over 48)
-// they are read twice.  Each stage is a round trip to memory or to LDS, and how many blocks a compute unit has under way decides:
+// they are read twice.  Attention-sink tokens (before `first`) have none: nothing reads them in this form, and what they hold
+// (an infinite residual, say) is to reach no sum.  Each stage is a round trip to memory or to LDS, and how many blocks a compute unit has under way decides:
 // 131072 tokens of 32 heads take 40 us with one block per workgroup, 31 with two, 35 with four; to LDS first and from there in
 // order to memory 32; 64 tokens' entries dealt out evenly, with a search for each lane's token, 69.
 constexpr int BT_HELD = 6, BT_SORT = 2;
 
 template <bool BLOCKED>
-__device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int n,
-                             int heads, uint32_t *start, uint32_t *list, uint32_t *count)
+__device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int first,
+                             int n, int heads, uint32_t *start, uint32_t *list, uint32_t *count)
 {
     const int tid = threadIdx.x, t = tid >> 3, l = tid & 7, lane = tid & 63, wave = tid >> 6;
     for (int h = tid; h < BT_SORT * heads; h += BT_NT) count[h] = 0u;
@@ -139,7 +140,7 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
     bool more = false;
 #pragma unroll
     for (int b = 0; b < BT_SORT; ++b) {
-        p1[b] = p1[b] < room ? p1[b] : room;
+        p1[b] = n0 + b * BT_BLOCK + t < first ? 0u : p1[b] < room ? p1[b] : room;
         more |= p1[b] > p0[b] + 8 * BT_HELD;
 #pragma unroll
         for (int i = 0; i < BT_HELD; ++i) {
@@ -245,6 +246,7 @@ __device__ void bt_query_row(const BtArgs &a, const KvqParamsHeader *hdr, int wh
     const float m = kvq_wave_max(__builtin_fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)));
     int e = 0;
     if (m > 0.0f && m < __builtin_inff()) (void)frexpf(m, &e);
+    e = e > -100 ? e : -100;                        // smaller ones have scores of nothing; a scale of zero would make NaN of a masked one
     x = ldexpf(x, 14 - e);
     y = ldexpf(y, 14 - e);
     const int64_t at = which == 0 ? ((int64_t)h * a.n_seqs + b) * a.ratio + r : (int64_t)row;
@@ -306,11 +308,11 @@ __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, i
     if (blk == 0 && values && i > 0)                // the workgroups of a sequence's own tokens find it by their number
         for (int c = tid; c < (g.n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK); c += BT_NT) a.w.owner[g.chunk0 + c] = i;
     uint32_t *start = (values ? a.w.v_start : a.w.k_start) + at, *list = values ? a.w.v_list + g.v_list : a.w.k_list + g.k_list;
-    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n, a.heads, start, list, count);
-    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n, a.heads, start, list, count);
+    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n_sink, g.n, a.heads, start, list, count);
+    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n_sink, g.n, a.heads, start, list, count);
     if (values && tid < BT_SORT * BT_BLOCK) {
         float m = 0.0f;
-        if (n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
+        if (n0 + tid >= g.n_sink && n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
         for (int d = 16; d; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
         if ((tid & 31) == 0 && n0 + tid < g.n) a.w.smax[g.blk0 + blk + (tid >> 5)] = m;
     }
@@ -1251,7 +1253,7 @@ __global__ __launch_bounds__(256) void kvq_batch_join(BtArgs a)
             o += sum[i][tid];
             w += weight[i];
         }
-        a.out[q0 + tid] = w > 0.0f ? o / w : 0.0f;
+        a.out[q0 + tid] = w == 0.0f ? 0.0f : o / w;          // (a NaN stays one)
     }
 }
 

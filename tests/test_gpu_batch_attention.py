@@ -211,6 +211,46 @@ def test_extreme_inputs(what):
     close(call(pre[1], both(per, 1), q), *reference(pre[0], both(per, 0), q, SCALE, wl.rope_base))
 
 
+@pytest.mark.parametrize("ratio", [2, 8])
+def test_what_a_sink_token_holds_in_codes_is_not_read(ratio):
+    """Sink tokens come from their fp16 rows: infinite residuals and scales in their compressed form reach no sum."""
+    import torch
+    wl = S.workload("c2", n_kv_heads=2, n_q_heads=2 * ratio)
+    sq = Seqs(Setup(wl))
+    pre = sq.make(300, n_sink=3)
+    per = [sq.make(40, seq=1 + i, n_sink=2, blocked=i == 1) for i in range(6)]
+    for oc, gc in [pre] + per:
+        n = int(gc.v_ptr[oc.n_sink].item())
+        assert n > 0
+        if gc.block_entries:
+            assert n <= gc.block_entries
+            gc.blocks["v_val"][0][:n] = 0x7C00
+            gc.blocks["k_val"][0][:int(gc.k_ptr[oc.n_sink].item())] = 0x7C00
+        else:
+            gc.v_val[:n] = 0x7C00
+            gc.k_val[:int(gc.k_ptr[oc.n_sink].item())] = 0x7C00
+        gc.v_sz[:2 * oc.n_sink] = 0x7C00
+    q = queries(wl, 6)
+    close(call(pre[1], both(per, 1), q), *reference(pre[0], both(per, 0), q, SCALE, wl.rope_base))
+
+
+@pytest.mark.parametrize("ratio", [1, 8])
+def test_smallest_queries_and_one_of_nan(ratio):
+    """Queries of zeros, of denormal numbers and of the largest ones with empty places beside them; a NaN stays in its own row."""
+    wl = S.workload("c2", n_kv_heads=2, n_q_heads=2 * ratio)
+    sq = Seqs(Setup(wl))
+    pre, per = sq.make(70), [sq.make(3 + i, seq=1 + i) for i in range(6)]
+    q = queries(wl, 6)
+    q[0], q[1], q[2] = 0.0, 1e-41, q[2] * 1e-35
+    q[4, 1, 77] = np.nan
+    clean = np.where(np.isnan(q), np.float32(0.0), q)
+    got = call(pre[1], both(per, 1), q).cpu()
+    ref, tol = reference(pre[0], both(per, 0), clean, SCALE, wl.rope_base)
+    assert got[4, 1].isnan().all()
+    got[4, 1], ref[4, 1] = 0.0, 0.0
+    close(got, ref, tol)
+
+
 def test_far_positions_of_own_tokens():
     """Own tokens behind a prefix of 70001: their Keys are rotated by that much more than their index says."""
     import torch
