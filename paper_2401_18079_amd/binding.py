@@ -69,7 +69,7 @@ def load_library():
         "kvq_attention_decode_batch": (C.c_int, [P, V, I32, V, F, V, V, I64, V]),
         "kvq_cache_copy": (C.c_int, [V, V, V, V, I32, V]),
         "kvq_cache_gather": (C.c_int, [P, P, V, I64, V]),
-        "kvq_cache_truncate": (C.c_int, [P, I64]),
+        "kvq_cache_truncate": (C.c_int, [V, I64]),
         "kvq_decode_step": (C.c_int, [P, V, V, V, F, V, I64, V, V]),
         "kvq_decode_step_launches": (I32, [P]),
         "kvq_softmax_workspace_bytes": (I64, [I32, I64]),
@@ -262,7 +262,7 @@ class KvqCache:
             else:
                 setattr(c, name, getattr(self, name).data_ptr())
         c.nnz_block_shift = self.block_entries.bit_length() - 1 if self.block_entries else 0
-        self.c = c
+        self.c, self.address = c, C.addressof(c)
         self.D, self.device = D, dev
         self.workspace = z(int(load_library().kvq_workspace_bytes(C.byref(c), max_append)), torch.uint8)
         c.workspace, c.workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
@@ -463,7 +463,7 @@ def kvq_attention_decode_noalloc(cache: KvqCache, q_rot: torch.Tensor, scale: fl
 
 def _cache_array(caches):
     """Host array of descriptor pointers (None: a null entry)."""
-    return (C.c_void_p * len(caches))(*[None if c is None else C.addressof(c.c) for c in caches])
+    return (C.c_void_p * len(caches))(*[None if c is None else c.address for c in caches])
 
 
 def kvq_attention_decode_batch_workspace_bytes(prefix, caches, n_seqs: int) -> int:
@@ -496,12 +496,11 @@ def kvq_attention_decode_batch(prefix, caches, q_rot: torch.Tensor, scale: float
 
 def kvq_cache_copy(dst, src, first=0, count=None, stream=None):
     """Appends tokens first .. first + count - 1 of src to dst (count None: all from `first` on).  dst and src: a KvqCache each, or
-    lists of the same length (one launch for a dozen copies); first and count: a number for all, or a list."""
+    lists of the same length (one launch for sixteen copies); first and count: a number for all, or a list."""
     one = isinstance(dst, KvqCache)
     ds, ss = ([dst], [src]) if one else (list(dst), list(src))
     n = len(ds)
-    assert len(ss) == n and all(isinstance(c, KvqCache) for c in ds + ss)
-    assert all(d.device == s.device for d, s in zip(ds, ss))
+    assert len(ss) == n and len({c.device for c in ds + ss}) <= 1
     f = [int(first)] * n if not isinstance(first, (list, tuple)) else [int(x) for x in first]
     if count is None:
         k = [s.n_tokens_k - x for s, x in zip(ss, f)]
@@ -522,7 +521,7 @@ def kvq_cache_gather(dst: KvqCache, src: KvqCache, tokens: torch.Tensor, stream=
 
 def kvq_cache_truncate(cache: KvqCache, n_tokens: int):
     """Drops the tokens from n_tokens on (host only)."""
-    _check(load_library().kvq_cache_truncate(C.byref(cache.c), int(n_tokens)), "kvq_cache_truncate")
+    _check((_lib or load_library()).kvq_cache_truncate(cache.address, int(n_tokens)), "kvq_cache_truncate")
 
 
 def kvq_softmax_f32(x: torch.Tensor, probs: torch.Tensor, n_cols: int, workspace: torch.Tensor, stream=None):

@@ -17,15 +17,13 @@ namespace {
 
 constexpr int MV_NT = 256;              // threads of a workgroup
 constexpr int MV_GROUP = 256;           // tokens of a workgroup of the outlier role
-constexpr int MV_JOBS = 12;             // copies whose descriptors travel in one launch's arguments
+constexpr int MV_JOBS = 16;             // copies whose descriptors travel in one launch's arguments: as many as 4 KiB hold
 
 struct MvSide {
     const uint32_t *s_ptr;
     uint32_t *d_ptr;
     const void *s_idx, *s_val;          // flat arrays, or tables of blocks (shift != 0)
     void *d_idx, *d_val;
-    uint32_t room;                      // the destination's capacity in entries
-    uint32_t pad;
 };
 
 struct MvJob {
@@ -34,14 +32,15 @@ struct MvJob {
     const uint32_t *s_sz;
     uint32_t *d_sz;
     MvSide k, v;
+    uint32_t k_room, v_room;            // the destination's capacity in entries
     int32_t *status;
     const uint16_t *s_sink_k, *s_sink_v;
     uint16_t *d_sink_k, *d_sink_v;
     const uint32_t *s_params;           // null: the destination has its constants
     uint32_t *d_params;
-    int32_t s_n, s_cap, d_cap, s_shift, d_shift;
+    int32_t s_n, s_cap, d_cap;
     int32_t first, at, n;               // source token of the first one, its place, how many
-    int32_t s_sink, d_sink;             // attention-sink tokens kept in fp16
+    int16_t s_shift, d_shift, s_sink, d_sink;       // of outlier blocks; attention-sink tokens kept in fp16
 };
 
 struct MvArgs {
@@ -49,7 +48,7 @@ struct MvArgs {
     int32_t wg0[MV_JOBS + 1];           // first workgroup of each
     MvJob job[MV_JOBS];
 };
-static_assert(sizeof(MvArgs) <= 4000, "kernel arguments");
+static_assert(sizeof(MvArgs) + 16 <= 4096 && KVQ_MAX_SINK < 32768, "kernel arguments");
 
 __host__ __device__ inline int mv_groups(int n) { return (n + MV_GROUP - 1) / MV_GROUP; }
 __host__ __device__ inline int mv_key_items(int at, int n) { return ((at + n + 63) >> 6) - (at >> 6); }
@@ -181,19 +180,19 @@ __device__ void mv_entries(const void *src, void *dst, int s_shift, int d_shift,
 }
 
 // A run's outliers of up to MV_GROUP tokens: pointers are the source's moved by a constant, entries a contiguous piece.
-__device__ void mv_run_side(const MvSide &a, int s_shift, int d_shift, int s0, int d0, int at, int first, int n, int32_t *status)
+__device__ void mv_run_side(const MvSide &a, uint32_t room, int s_shift, int d_shift, int s0, int d0, int at, int first, int n, int32_t *status)
 {
     const uint32_t base = a.d_ptr[at], from = a.s_ptr[first];
     const int tid = threadIdx.x;
     bool over = false;
     auto place = [&](uint32_t s) {                          // where the destination's entries end for a source pointer
         const uint64_t e = (uint64_t)base + (s - from);
-        return e < a.room ? (uint32_t)e : a.room;
+        return e < room ? (uint32_t)e : room;
     };
     const uint32_t p0 = a.s_ptr[s0], e0 = place(p0), e1 = place(a.s_ptr[s0 + n]);
     if (tid < n) {
         const uint32_t s = a.s_ptr[s0 + tid + 1];
-        over = (uint64_t)base + (s - from) > a.room;
+        over = (uint64_t)base + (s - from) > room;
         a.d_ptr[d0 + tid + 1] = place(s);
     }
     mv_entries(a.s_idx, a.d_idx, s_shift, d_shift, p0, e0, e1 - e0);
@@ -237,7 +236,7 @@ __global__ __launch_bounds__(MV_NT) void kvq_move(MvArgs a, const int32_t *__res
         const int i0 = (LIST ? wg : wg >> 1) * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
         if (LIST || (wg & 1)) mv_scales<LIST>(j, tokens, a.heads, i0, n);
         if (!LIST) {
-            mv_run_side((wg & 1) ? j.v : j.k, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
+            mv_run_side((wg & 1) ? j.v : j.k, (wg & 1) ? j.v_room : j.k_room, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
         } else {
             __shared__ uint32_t part[MV_NT / 64][2];
             const int t = tid < n ? mv_source<true>(j, tokens, i0 + tid) : -1;
@@ -285,6 +284,7 @@ __global__ __launch_bounds__(MV_NT) void kvq_move_lists(MvArgs a, const int32_t 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int side = blockIdx.x & 1, quarter = (blockIdx.x >> 1) & 3, wg = blockIdx.x >> 3;
     const MvSide &s = side == 0 ? j.k : j.v;
+    const uint32_t room = side == 0 ? j.k_room : j.v_room;
     const int i0 = wg * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
     if (quarter * MV_PART >= n) return;
     const int t = tid < n ? mv_source<true>(j, tokens, i0 + tid) : -1;
@@ -305,13 +305,13 @@ __global__ __launch_bounds__(MV_NT) void kvq_move_lists(MvArgs a, const int32_t 
     const uint64_t base = (uint64_t)s.d_ptr[j.at] + wave_sum[0][0] + wave_sum[0][1] + wave_sum[0][2] + wave_sum[0][3];
     for (int w = 0; w < wave; ++w) sum += wave_sum[1][w];
     const uint64_t end = base + sum;
-    const uint32_t clipped = end < s.room ? (uint32_t)end : s.room;
-    begin[tid] = end - c < s.room ? (uint32_t)(end - c) : s.room;
+    const uint32_t clipped = end < room ? (uint32_t)end : room;
+    begin[tid] = end - c < room ? (uint32_t)(end - c) : room;
     from[tid] = p;
     if (tid == MV_GROUP - 1) begin[MV_GROUP] = clipped;
     if (tid < n && wave == quarter) {
         s.d_ptr[j.at + i0 + tid + 1] = clipped;
-        if (end > s.room) atomicExch(j.status, (int32_t)KVQ_ERR_NNZ_OVERFLOW);
+        if (end > room) atomicExch(j.status, (int32_t)KVQ_ERR_NNZ_OVERFLOW);
     }
     __syncthreads();
     const int last = (quarter + 1) * MV_PART < n ? (quarter + 1) * MV_PART : n;
@@ -357,7 +357,7 @@ void mv_job(MvJob &j, const kvq_cache *dst, const kvq_cache *src, int64_t first,
     memset(&j, 0, sizeof j);
     j.s_kc = src->k_codes; j.s_vc = src->v_codes; j.d_kc = dst->k_codes; j.d_vc = dst->v_codes;
     j.s_sz = (const uint32_t *)src->v_sz; j.d_sz = (uint32_t *)dst->v_sz;
-    j.s_shift = src->nnz_block_shift; j.d_shift = dst->nnz_block_shift;
+    j.s_shift = (int16_t)src->nnz_block_shift; j.d_shift = (int16_t)dst->nnz_block_shift;
     j.k.s_ptr = src->k_ptr; j.k.d_ptr = dst->k_ptr; j.v.s_ptr = src->v_ptr; j.v.d_ptr = dst->v_ptr;
     j.k.s_idx = j.s_shift ? (const void *)src->k_idx_blocks : src->k_idx;
     j.k.s_val = j.s_shift ? (const void *)src->k_val_blocks : src->k_val;
@@ -367,8 +367,8 @@ void mv_job(MvJob &j, const kvq_cache *dst, const kvq_cache *src, int64_t first,
     j.k.d_val = j.d_shift ? (void *)dst->k_val_blocks : dst->k_val;
     j.v.d_idx = j.d_shift ? (void *)dst->v_idx_blocks : dst->v_idx;
     j.v.d_val = j.d_shift ? (void *)dst->v_val_blocks : dst->v_val;
-    j.k.room = (uint32_t)(dst->cap_nnz_k < 0xFFFFFFFFll ? dst->cap_nnz_k : 0xFFFFFFFFll);
-    j.v.room = (uint32_t)(dst->cap_nnz_v < 0xFFFFFFFFll ? dst->cap_nnz_v : 0xFFFFFFFFll);
+    j.k_room = (uint32_t)(dst->cap_nnz_k < 0xFFFFFFFFll ? dst->cap_nnz_k : 0xFFFFFFFFll);
+    j.v_room = (uint32_t)(dst->cap_nnz_v < 0xFFFFFFFFll ? dst->cap_nnz_v : 0xFFFFFFFFll);
     j.status = dst->d_status;
     j.s_sink_k = src->sink_k; j.s_sink_v = src->sink_v; j.d_sink_k = dst->sink_k; j.d_sink_v = dst->sink_v;
     if (!dst->loaded) {
@@ -378,7 +378,7 @@ void mv_job(MvJob &j, const kvq_cache *dst, const kvq_cache *src, int64_t first,
     j.s_n = (int32_t)(src->n_tokens_k < src->n_tokens_v ? src->n_tokens_k : src->n_tokens_v);
     j.s_cap = (int32_t)src->cap_tokens; j.d_cap = (int32_t)dst->cap_tokens;
     j.first = (int32_t)first; j.at = (int32_t)dst->n_tokens_k; j.n = (int32_t)n;
-    j.s_sink = src->n_sink; j.d_sink = dst->n_sink;
+    j.s_sink = (int16_t)src->n_sink; j.d_sink = (int16_t)dst->n_sink;
 }
 
 int64_t mv_wgs(const MvJob &j, int heads, int param_words, bool list)
@@ -419,12 +419,12 @@ extern "C" kvq_status kvq_cache_copy(kvq_cache *const *dst, const kvq_cache *con
         // sink tokens have their fp16 rows only where they are sink tokens of the source
         const int64_t at = dst[i]->n_tokens_k, sinks = dst[i]->n_sink - at < count[i] ? dst[i]->n_sink - at : count[i];
         if (sinks > 0 && first[i] + sinks > src[i]->n_sink) return KVQ_ERR_INVALID_ARG;
-        for (int32_t k = 0; k < n_copies; ++k) {
-            if (dst[i] == src[k] || (src[k] && dst[i]->k_codes == src[k]->k_codes)) return KVQ_ERR_INVALID_ARG;
-            if (k < i && (dst[i] == dst[k] || dst[i]->k_codes == dst[k]->k_codes)) return KVQ_ERR_INVALID_ARG;
-            if (dst[k] && (dst[k]->bits != dst[i]->bits || dst[k]->n_kv_heads != dst[i]->n_kv_heads)) return KVQ_ERR_INVALID_ARG;
-        }
+        if (dst[i]->bits != dst[0]->bits || dst[i]->n_kv_heads != dst[0]->n_kv_heads) return KVQ_ERR_INVALID_ARG;
     }
+    // no destination is another's source or destination as well
+    for (int32_t i = 0; i < n_copies; ++i)
+        for (int32_t k = 0; k < n_copies; ++k)
+            if (dst[i]->k_codes == src[k]->k_codes || (k < i && dst[i]->k_codes == dst[k]->k_codes)) return KVQ_ERR_INVALID_ARG;
     MvArgs a;
     memset(&a, 0, sizeof a);
     int64_t wgs = 0;
