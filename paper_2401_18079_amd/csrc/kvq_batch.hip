@@ -113,37 +113,44 @@ __device__ __forceinline__ uint32_t bt_entry(const void *arr, int shift, uint32_
     return bt_global(((const uint16_t *const *)arr)[e >> shift])[e & ((1u << shift) - 1u)];
 }
 
-// The entries of two blocks of 32 tokens sorted by block and head: eight lanes a token, an entry's rank among its head's from the count
+// The entries of SORT blocks of 32 tokens sorted by block and head: eight lanes a token, an entry's rank among its head's from the count
 // that it adds to, its place from the sums of the counts.  (The order within a head is any: every entry has an element of its own.)
-// A lane keeps up to BT_HELD entries of each block in registers from the count to the placing; where a token has more (over 48)
-// they are read twice.  Attention-sink tokens (before `first`) have none: nothing reads them in this form, and what they hold
-// (an infinite residual, say) is to reach no sum.  Each stage is a round trip to memory or to LDS, and how many blocks a compute unit has under way decides:
-// 131072 tokens of 32 heads take 40 us with one block per workgroup, 31 with two, 35 with four; to LDS first and from there in
-// order to memory 32; 64 tokens' entries dealt out evenly, with a search for each lane's token, 69.
-constexpr int BT_HELD = 6, BT_SORT = 2;
+// A lane keeps up to HELD entries of each block in registers from the count to the placing; where a token has more they are read
+// twice.  Attention-sink tokens (before `first`) have none: nothing reads them in this form, and what they hold (an infinite
+// residual, say) is to reach no sum.
+// Each stage is a round trip to memory or to LDS, and how many blocks a compute unit has under way decides: 131072 tokens of 32
+// heads take 40 us with one block per workgroup, 31 with two, 35 with four; to LDS first and from there in order to memory 32; 64
+// tokens' entries dealt out evenly, with a search for each lane's token, 69.  Layers of few heads have few entries a token:
+// 524287 tokens of 8 heads take 76 us with two blocks, 62 with four of half the registers, 57 with eight, which take 8 us for 300
+// tokens where the others take 6.
+constexpr int BT_HELD = 6, BT_SORT = 2, BT_HELD_FEW = 3, BT_SORT_FEW = 4, BT_FEW_HEADS = 16;
 
-template <bool BLOCKED>
+template <bool BLOCKED, int SORT, int HELD>
 __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *val, int shift, uint32_t room, int n0, int first,
                              int n, int heads, uint32_t *start, uint32_t *list, uint32_t *count)
 {
     const int tid = threadIdx.x, t = tid >> 3, l = tid & 7, lane = tid & 63, wave = tid >> 6;
-    for (int h = tid; h < BT_SORT * heads; h += BT_NT) count[h] = 0u;
-    uint32_t p0[BT_SORT], p1[BT_SORT], x[BT_SORT][BT_HELD], v[BT_SORT][BT_HELD], rank[BT_SORT][BT_HELD];
-    const int my_first = n0 + wave * BT_BLOCK;                   // first token of the block whose sums this wavefront takes
-    const uint32_t base = my_first < n ? ptr[my_first] : 0u;
+    for (int h = tid; h < SORT * heads; h += BT_NT) count[h] = 0u;
+    uint32_t p0[SORT], p1[SORT], x[SORT][HELD], v[SORT][HELD], rank[SORT][HELD];
+    uint32_t base[(SORT + BT_WAVES - 1) / BT_WAVES];             // first entries of the blocks whose sums this wavefront takes
 #pragma unroll
-    for (int b = 0; b < BT_SORT; ++b) {
+    for (int k = 0; k < (SORT + BT_WAVES - 1) / BT_WAVES; ++k) {
+        const int m = n0 + (wave + k * BT_WAVES) * BT_BLOCK;
+        base[k] = ptr[m < n ? m : n];
+    }
+#pragma unroll
+    for (int b = 0; b < SORT; ++b) {
         const int m = n0 + b * BT_BLOCK + t;
         p0[b] = ptr[m < n ? m : n];
         p1[b] = ptr[m < n ? m + 1 : n];
     }
     bool more = false;
 #pragma unroll
-    for (int b = 0; b < BT_SORT; ++b) {
+    for (int b = 0; b < SORT; ++b) {
         p1[b] = n0 + b * BT_BLOCK + t < first ? 0u : p1[b] < room ? p1[b] : room;
-        more |= p1[b] > p0[b] + 8 * BT_HELD;
+        more |= p1[b] > p0[b] + 8 * HELD;
 #pragma unroll
-        for (int i = 0; i < BT_HELD; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             const uint32_t e = p0[b] + l + 8 * i;
             if (e < p1[b]) {
                 x[b][i] = bt_entry<BLOCKED>(idx, shift, e);
@@ -152,19 +159,19 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
         }
     }
 #pragma unroll
-    for (int b = 0; b < BT_SORT; ++b)
+    for (int b = 0; b < SORT; ++b)
 #pragma unroll
-        for (int i = 0; i < BT_HELD; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             asm volatile("" : "+v"(v[b][i]));
             x[b][i] |= v[b][i] << 16;
         }
     const bool many = __syncthreads_or(more) != 0;
 #pragma unroll
-    for (int b = 0; b < BT_SORT; ++b) {
+    for (int b = 0; b < SORT; ++b) {
         uint32_t *const mine = count + b * heads;
         if (!many) {
 #pragma unroll
-            for (int i = 0; i < BT_HELD; ++i)
+            for (int i = 0; i < HELD; ++i)
                 if (p0[b] + l + 8 * i < p1[b] && ((x[b][i] & 0xFFFFu) >> 7) < (uint32_t)heads) rank[b][i] = atomicAdd(&mine[(x[b][i] & 0xFFFFu) >> 7], 1u);
         } else {
             for (uint32_t e = p0[b] + l; e < p1[b]; e += 8) {
@@ -174,8 +181,11 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
         }
     }
     __syncthreads();
-    if (wave < BT_SORT) {                           // exclusive sums, a wavefront a block, up to eight heads a lane
-        uint32_t c[BT_MAX_HEADS / 64], s = 0, *const mine = count + wave * heads;
+#pragma unroll
+    for (int k = 0; k < (SORT + BT_WAVES - 1) / BT_WAVES; ++k) {            // exclusive sums, a wavefront a block, up to eight heads a lane
+        const int b = wave + k * BT_WAVES;
+        if (b >= SORT) break;
+        uint32_t c[BT_MAX_HEADS / 64], s = 0, *const mine = count + b * heads;
         const int per = (heads + 63) / 64;
 #pragma unroll
         for (int i = 0; i < BT_MAX_HEADS / 64; ++i) {
@@ -188,15 +198,15 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
             const uint32_t o = (uint32_t)__shfl_up((int)before, d);
             if (lane >= d) before += o;
         }
-        before += base - s;
+        before += base[k] - s;
 #pragma unroll
         for (int i = 0; i < BT_MAX_HEADS / 64; ++i) {
             const int h = lane * per + i;
             if (i < per && h < heads) {
                 mine[h] = before;
-                if (my_first < n) {
-                    start[wave * (heads + 1) + h] = before;
-                    if (h == heads - 1) start[wave * (heads + 1) + heads] = before + c[i];
+                if (n0 + b * BT_BLOCK < n) {
+                    start[b * (heads + 1) + h] = before;
+                    if (h == heads - 1) start[b * (heads + 1) + heads] = before + c[i];
                 }
                 before += c[i];
             }
@@ -204,11 +214,11 @@ __device__ void bt_sort_side(const uint32_t *ptr, const void *idx, const void *v
     }
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < BT_SORT; ++b) {
+    for (int b = 0; b < SORT; ++b) {
         uint32_t *const mine = count + b * heads;
         if (!many) {
 #pragma unroll
-            for (int i = 0; i < BT_HELD; ++i) {
+            for (int i = 0; i < HELD; ++i) {
                 const uint32_t c = x[b][i] & 0xFFFFu;
                 if (p0[b] + l + 8 * i < p1[b] && (c >> 7) < (uint32_t)heads) {
                     const uint32_t at = mine[c >> 7] + rank[b][i];
@@ -268,11 +278,12 @@ __device__ __forceinline__ void bt_upload(const BtArgs &a, const BtSegs &s)
 }
 __global__ __launch_bounds__(BT_NT) void kvq_batch_upload(BtArgs a, BtSegs s) { bt_upload(a, s); }
 
-// First kernel: query rows; outliers by head, BT_SORT blocks of 32 tokens and a side per workgroup.  A call whose descriptors fit in the
+// First kernel: query rows; outliers by head, SORT blocks of 32 tokens and a side per workgroup.  A call whose descriptors fit in the
 // arguments brings them along; otherwise (`total` > s.n) they are in memory already.
+template <int SORT, int HELD>
 __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, int row_wgs, int total)
 {
-    __shared__ uint32_t count[BT_SORT * BT_MAX_HEADS];
+    __shared__ uint32_t count[SORT * (SORT == BT_SORT ? BT_MAX_HEADS : BT_FEW_HEADS)];
     const int tid = threadIdx.x, lane = tid & 63;
     int wg = blockIdx.x;
     if (wg == 0 && total == s.n) bt_upload(a, s);
@@ -299,7 +310,7 @@ __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, i
         i = __builtin_amdgcn_readfirstlane(found) - 1;
     }
     const BtSeg g = total == s.n ? bt_seg(s.seg[i]) : bt_seg(a.w.segs[i]);
-    const int blk = BT_SORT * (wg - g.wg0), n0 = blk * BT_BLOCK;
+    const int blk = SORT * (wg - g.wg0), n0 = blk * BT_BLOCK;
     if (n0 >= g.n) return;
     const int64_t at = (int64_t)(g.blk0 + blk) * (a.heads + 1);
     const uint32_t *ptr = values ? g.v_ptr : g.k_ptr;
@@ -308,9 +319,9 @@ __global__ __launch_bounds__(BT_NT) void kvq_batch_prepare(BtArgs a, BtSegs s, i
     if (blk == 0 && values && i > 0)                // the workgroups of a sequence's own tokens find it by their number
         for (int c = tid; c < (g.n + a.chunk[1] * BT_BLOCK - 1) / (a.chunk[1] * BT_BLOCK); c += BT_NT) a.w.owner[g.chunk0 + c] = i;
     uint32_t *start = (values ? a.w.v_start : a.w.k_start) + at, *list = values ? a.w.v_list + g.v_list : a.w.k_list + g.k_list;
-    if (g.shift == 0) bt_sort_side<false>(ptr, idx, val, 0, room, n0, g.n_sink, g.n, a.heads, start, list, count);
-    else bt_sort_side<true>(ptr, idx, val, g.shift, room, n0, g.n_sink, g.n, a.heads, start, list, count);
-    if (values && tid < BT_SORT * BT_BLOCK) {
+    if (g.shift == 0) bt_sort_side<false, SORT, HELD>(ptr, idx, val, 0, room, n0, g.n_sink, g.n, a.heads, start, list, count);
+    else bt_sort_side<true, SORT, HELD>(ptr, idx, val, g.shift, room, n0, g.n_sink, g.n, a.heads, start, list, count);
+    if (values && tid < SORT * BT_BLOCK) {
         float m = 0.0f;
         if (n0 + tid >= g.n_sink && n0 + tid < g.n) m = __builtin_fabsf(kvq_h2f((uint16_t)(g.v_sz[n0 + tid] & 0xFFFFu)));
         for (int d = 16; d; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
@@ -1467,6 +1478,7 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
     // ---- descriptors, BT_SEGS at a time in the arguments of the first kernel
     BtSegs part;
     int64_t k_list = 0, v_list = 0, blk = 0, chunk = 0, wgs = 0;
+    const int sort = one->n_kv_heads <= BT_FEW_HEADS ? BT_SORT_FEW : BT_SORT;
     memset(&part, 0, sizeof part);
     for (int32_t i = 0; i <= n_seqs; ++i) {
         const kvq_cache *c = i == 0 ? prefix : caches ? caches[i - 1] : nullptr;
@@ -1503,7 +1515,7 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
             v_list += vr;
             const int64_t nb = (c->n_tokens_k + BT_BLOCK - 1) / BT_BLOCK;
             blk += nb;
-            wgs += (nb + BT_SORT - 1) / BT_SORT;
+            wgs += (nb + sort - 1) / sort;
             if (i > 0) chunk += (nb + a.chunk[1] - 1) / a.chunk[1];
         }
         if (++part.n < BT_SEGS && i < n_seqs) continue;
@@ -1518,7 +1530,9 @@ extern "C" kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const 
     }
     const int64_t row_wgs = ((int64_t)n_seqs * one->n_q_heads + BT_WAVES - 1) / BT_WAVES;
     if (row_wgs + 2 * wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
-    kvq_batch_prepare<<<dim3((unsigned)(row_wgs + 2 * wgs)), dim3(BT_NT), 0, s>>>(a, part, (int)row_wgs, n_seqs + 1);
+    const dim3 grid((unsigned)(row_wgs + 2 * wgs)), block(BT_NT);
+    if (sort == BT_SORT) kvq_batch_prepare<BT_SORT, BT_HELD><<<grid, block, 0, s>>>(a, part, (int)row_wgs, n_seqs + 1);
+    else kvq_batch_prepare<BT_SORT_FEW, BT_HELD_FEW><<<grid, block, 0, s>>>(a, part, (int)row_wgs, n_seqs + 1);
     KVQ_HIP_CHECK(hipGetLastError());
     st = bt_launch(p, one->bits, s);
     if (st != KVQ_OK) return st;
