@@ -62,8 +62,8 @@ typedef enum {
 
 /*
  * One layer's cache for one sequence.  Plain data, owned by the caller, lives in HOST memory;
- * the pointers inside are DEVICE pointers, each 16-byte aligned.  A batch of independent
- * sequences is an array of these (one call per sequence).
+ * the pointers inside are DEVICE pointers, each 16-byte aligned.  A batch of
+ * sequences is an array of these (one call per sequence; kvq_attention_decode_batch takes them all).
  */
 typedef struct kvq_cache {
     int32_t bits;           /* 2, 3 or 4                                                        */
@@ -299,8 +299,8 @@ kvq_status kvq_attention_decode_noalloc(const kvq_cache *cache, const float *d_q
  *   out[b][q][c] = sum_n softmax_n(x[b][q][.])[n] * vhat[n][kv(q)*128 + c],
  *   x[b][q][n] = scale * sum_c q_rot[b][q][c] * RoPE_n(khat[n][kv(q)])[c],
  * n over the tokens of `prefix` (positions 0 .. P-1) and then those of caches[b] (its token j at position P + j), khat and
- * vhat as defined for kvq_qk_matvec and kvq_pv_matvec.  The prefix is read, de-quantised and rotated once for 64 queries
- * of a KV head at a time, whatever sequences they belong to.
+ * vhat as defined for kvq_qk_matvec and kvq_pv_matvec.  The prefix is read, de-quantised and rotated once for up to 128
+ * queries of a KV head at a time, whatever sequences they belong to.
  *   prefix   : the shared tokens, or NULL (a batch of unrelated sequences; P = 0).
  *   caches   : HOST array of n_seqs caches, or NULL (no sequence has tokens of its own); a NULL entry is a sequence without
  *              tokens of its own.  The same cache may be listed more than once, and `prefix` among them: nothing is written
@@ -313,7 +313,8 @@ kvq_status kvq_attention_decode_noalloc(const kvq_cache *cache, const float *d_q
  *   d_workspace : DEVICE, 16-byte aligned, kvq_attention_decode_batch_workspace_bytes() bytes for the same arguments and token
  *              counts (0: the arguments are not usable).  It grows with the tokens: 4 bytes per outlier entry above all.
  * The matrix products take fp16 factors in two parts with fp32 sums: results agree with kvq_attention_decode on the joined
- * sequence to fp32 rounding, and are run-to-run identical.  The descriptors are read during the call: token counts are those
+ * sequence to fp32 rounding, and are run-to-run identical.  The parts end at 2^-24 of a Key's element (the rounding of those
+ * below 1/64) and, for Value scales below 1, at 2^-33 of the largest weight; scales below 2^e raise that to 2^(e-33).  The descriptors are read during the call: token counts are those
  * of the call, also where it is captured into a graph.  Calls that share a workspace must not overlap.
  * Errors: INVALID_ARG, UNSUPPORTED, NOT_LOADED, CAPACITY (workspace), HIP.
  */
@@ -341,7 +342,7 @@ kvq_status kvq_attention_decode_batch(const kvq_cache *prefix, const kvq_cache *
  * Both caches of a pair have the same bits, n_kv_heads and rope_base; all destinations of one copy the same bits and
  * n_kv_heads.  Capacities, outlier storage (flat or blocked), k_side_v and n_q_heads may differ.  The destination has
  * n_tokens_k == n_tokens_v (they advance together); a source needs the copied tokens on both sides, for a gather also
- * n_tokens_k == n_tokens_v.  The constants of kvq_lut_load: a destination that has not been loaded must be empty and takes over the
+ * n_tokens_k == n_tokens_v.  Token counts are those of the call, also where it is captured into a graph.  The constants of kvq_lut_load: a destination that has not been loaded must be empty and takes over the
  * source's (params is copied on `stream`, loaded is set); one that has been keeps its own, which are the caller's to be the
  * same.  Attention-sink tokens: a token that lands below dst->n_sink must be one of the source's (its fp16 row is copied;
  * INVALID_ARG otherwise, for a gather through *d_status, with a zero row); one that lands elsewhere goes on with its codes.

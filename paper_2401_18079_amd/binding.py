@@ -343,7 +343,8 @@ class KvqCache:
 
     def free_nnz_blocks(self) -> int:
         """Blocked storage: gives back the blocks behind the entries in use (after kvq_cache_truncate), keeping one per array.
-        Returns how many blocks.  Synchronises, since work that reads them may be under way."""
+        Returns how many blocks.  Synchronises, since work that reads them may be under way.  Appends and copies into this cache
+        that were captured into a graph before hold the old capacity: they are to be captured again."""
         if not self.block_entries:
             return 0
         freed = 0

@@ -540,14 +540,15 @@ __device__ __forceinline__ uint32_t bt_key_field(const uint32_t (&w)[BITS], int 
 // Running sums of MB blocks of 16 queries: a query per column of the lanes, in log2 units with its own maximum.
 template <int MB>
 struct BtSums {
-    float4_t o[8][MB], lz[MB];          // output by channel block; (sum of p z, sum of p) in the first lanes' first two
+    float4_t o[8][MB];                  // output by channel block
+    float2_t lz[MB];                    // (sum of p z, sum of p) in the first 16 lanes
     float m[MB], inv[MB];
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             m[mb] = KVQ_STAT_FLOOR;
-            lz[mb] = float4_t{0.f, 0.f, 0.f, 0.f};
+            lz[mb] = float2_t{0.f, 0.f};
 #pragma unroll
             for (int cb = 0; cb < 8; ++cb) o[cb][mb] = float4_t{0.f, 0.f, 0.f, 0.f};
         }
@@ -591,13 +592,16 @@ __device__ __forceinline__ void bt_maximum(const float4_t (&s)[GROUPS][2][MB], B
     if (__ballot(m > sum.m[mb] + BT_MAX_SLACK) != 0ull) {
         const float up = m > sum.m[mb] ? m : sum.m[mb], f = __builtin_amdgcn_exp2f(sum.m[mb] - up);
         sum.m[mb] = up;
-        sum.lz[mb] *= f;
+        sum.lz[mb].x *= f;
+        sum.lz[mb].y *= f;
 #pragma unroll
         for (int cb = 0; cb < 8; ++cb) sum.o[cb][mb] *= f;
     }
 }
 
-// Scores of 32 tokens to weights, and the sums of p z and of p (a channel block of their own with rows (z, 1, 0 ...)).
+// Scores of 32 tokens to weights, and the sums of p z and of p (a channel block of their own with rows (z, 1, 0 ...)).  These two grow
+// with every token: they are taken from zero for 32 tokens and added in fp32, which rounds to nearest.  (Left in the products'
+// own sums, whose error has a direction, 524287 tokens came out 3.4e-6 to 5.2e-6 off, now 2.0e-6 to 2.4e-6; the time is the same.)
 template <int MB>
 __device__ __forceinline__ void bt_weights(const float4_t (&s)[2][MB], const uint32_t (&sz)[2][4], BtSums<MB> &sum, BtWeights (&w)[MB], int r16,
                                            float kap, float minus_one)
@@ -630,8 +634,9 @@ __device__ __forceinline__ void bt_weights(const float4_t (&s)[2][MB], const uin
     const half8_t zf = bt_half8(x[0], x[1], x[2], x[3]);
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
-        sum.lz[mb] = bt_mfma(zf, w[mb].pl, sum.lz[mb]);
-        sum.lz[mb] = bt_mfma(zf, w[mb].ph, sum.lz[mb]);
+        const float4_t t = bt_mfma(zf, w[mb].ph, bt_mfma(zf, w[mb].pl, float4_t{0.f, 0.f, 0.f, 0.f}));
+        sum.lz[mb].x += t[0];
+        sum.lz[mb].y += t[1];
     }
 }
 
@@ -856,7 +861,7 @@ __device__ __forceinline__ void BtAlone<BITS, MB, WHICH>::run(const BtArgs &a, i
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             wave_m[wave][mb * 16 + r16] = sum.m[mb];
-            wave_l[wave][mb * 16 + r16] = sum.lz[mb][1];
+            wave_l[wave][mb * 16 + r16] = sum.lz[mb].y;
         }
     __syncthreads();
     const int64_t slot0 = ((int64_t)p.ch * a.heads + p.h) * a.mp[WHICH] + (int64_t)p.qb * 16 * MB;
@@ -864,7 +869,7 @@ __device__ __forceinline__ void BtAlone<BITS, MB, WHICH>::run(const BtArgs &a, i
     for (int mb = 0; mb < MB; ++mb) {
         const int c = mb * 16 + r16;
         const float m = __builtin_fmaxf(__builtin_fmaxf(wave_m[0][c], wave_m[1][c]), __builtin_fmaxf(wave_m[2][c], wave_m[3][c]));
-        const float fac = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap), z = __shfl(sum.lz[mb][0], r16);
+        const float fac = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap), z = __shfl(sum.lz[mb].x, r16);
         if (mb > 0) __syncthreads();
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
@@ -1125,7 +1130,7 @@ __device__ __forceinline__ void BtTogether<BITS, QW, WHICH>::run(const BtArgs &a
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
                 wave_m[wave][mb * 16 + r16] = sum.m[mb];
-                wave_l[wave][mb * 16 + r16] = sum.lz[mb][1];
+                wave_l[wave][mb * 16 + r16] = sum.lz[mb].y;
             }
         __syncthreads();
     }
@@ -1137,13 +1142,13 @@ __device__ __forceinline__ void BtTogether<BITS, QW, WHICH>::run(const BtArgs &a
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
                 const int c = mb * 16 + r16;
-                float m = sum.m[mb], l = sum.lz[mb][1];
+                float m = sum.m[mb], l = sum.lz[mb].y;
                 if (TW == 2) {
                     m = __builtin_fmaxf(wave_m[qg][c], wave_m[(QW + qg) % BT_WAVES][c]);
                     l = wave_l[qg][c] * __builtin_amdgcn_exp2f(wave_m[qg][c] - m) +
                         wave_l[(QW + qg) % BT_WAVES][c] * __builtin_amdgcn_exp2f(wave_m[(QW + qg) % BT_WAVES][c] - m);
                 }
-                const float fac = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap), z = __shfl(sum.lz[mb][0], r16);
+                const float fac = __builtin_amdgcn_exp2f(sum.m[mb] - m - kap), z = __shfl(sum.lz[mb].x, r16);
                 const bool in = q0 + c < p.n_q;
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
