@@ -8,7 +8,8 @@
 //           their halves of every field put together with a shift of the whole chunk by one code.
 //   outliers, scales and pointers: 256 tokens a workgroup, a run's entries as one contiguous piece.
 // A run's pointers are the source's plus a constant, so a copy is one launch; a list's need the sum of the counts before
-// them, which the first of two launches leaves per 256 tokens.
+// them, which the first of two launches, a short one, leaves per 256 tokens.  (32768 of 131072 tokens of 32 heads: 145 us with the
+// codes in the first launch and the lists alone in the second, 133 so.)
 #include <string.h>
 #include "kvq_append_keys.hpp"
 #include "kvq_common.hpp"
@@ -222,67 +223,38 @@ __device__ void mv_scales(const MvJob &j, const int32_t *tokens, int heads, int 
     }
 }
 
-// The kernel of a copy, and the first of a gather (LIST), which leaves the counts of every MV_GROUP tokens in `sums`.
-template <int BITS, bool LIST>
-__global__ __launch_bounds__(MV_NT) void kvq_move(MvArgs a, const int32_t *__restrict__ tokens, uint32_t *__restrict__ sums)
+// First kernel of a gather: the counts of every MV_GROUP listed tokens.
+__global__ __launch_bounds__(MV_NT) void kvq_move_counts(MvJob j, const int32_t *__restrict__ tokens, uint32_t *__restrict__ sums)
 {
-    int wg = blockIdx.x, i = 0;
-    while (i + 1 < a.n_jobs && wg >= a.wg0[i + 1]) ++i;
-    const MvJob &j = a.job[i];
-    wg -= a.wg0[i];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int groups = mv_groups(j.n) * (LIST ? 1 : 2);
-    if (wg < groups) {
-        const int i0 = (LIST ? wg : wg >> 1) * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
-        if (LIST || (wg & 1)) mv_scales<LIST>(j, tokens, a.heads, i0, n);
-        if (!LIST) {
-            mv_run_side((wg & 1) ? j.v : j.k, (wg & 1) ? j.v_room : j.k_room, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
-        } else {
-            __shared__ uint32_t part[MV_NT / 64][2];
-            const int t = tid < n ? mv_source<true>(j, tokens, i0 + tid) : -1;
-            uint32_t k = t < 0 ? 0u : j.k.s_ptr[t + 1] - j.k.s_ptr[t], v = t < 0 ? 0u : j.v.s_ptr[t + 1] - j.v.s_ptr[t];
-            for (int d = 32; d; d >>= 1) {
-                k += (uint32_t)__shfl_xor((int)k, d);
-                v += (uint32_t)__shfl_xor((int)v, d);
-            }
-            if (lane == 0) {
-                part[wave][0] = k;
-                part[wave][1] = v;
-            }
-            __syncthreads();
-            if (tid < 2) sums[2 * wg + tid] = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
-        }
-        return;
+    __shared__ uint32_t part[MV_NT / 64][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x * MV_GROUP + tid;
+    const int t = i < j.n ? mv_source<true>(j, tokens, i) : -1;
+    uint32_t k = t < 0 ? 0u : j.k.s_ptr[t + 1] - j.k.s_ptr[t], v = t < 0 ? 0u : j.v.s_ptr[t + 1] - j.v.s_ptr[t];
+    for (int d = 32; d; d >>= 1) {
+        k += (uint32_t)__shfl_xor((int)k, d);
+        v += (uint32_t)__shfl_xor((int)v, d);
     }
-    wg -= groups;
-    if (j.s_params) {
-        const int wgs = (a.param_words + 16 * MV_NT - 1) / (16 * MV_NT);
-        if (wg < wgs) {
-            for (int w = wg * 16 * MV_NT + tid; w < a.param_words && w < (wg + 1) * 16 * MV_NT; w += MV_NT) j.d_params[w] = j.s_params[w];
-            return;
-        }
-        wg -= wgs;
+    if (lane == 0) {
+        part[wave][0] = k;
+        part[wave][1] = v;
     }
-    const int key_items = mv_key_items(j.at, j.n) * a.heads, value_items = 2 * mv_value_items(j.at, j.n) * a.heads;
-    const int key_wgs = (key_items + 3) / 4;
-    if (wg < key_wgs) {
-        const int item = wg * 4 + wave;
-        if (item < key_items) mv_keys<BITS, LIST>(j, tokens, item, lane);
-    } else {
-        const int item = (wg - key_wgs) * 4 + wave;
-        if (item < value_items) mv_values<BITS, LIST>(j, tokens, item, lane);
-    }
+    __syncthreads();
+    if (tid < 2) sums[2 * blockIdx.x + tid] = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
 }
 
-// Second kernel of a gather: pointers and entries of MV_PART listed tokens, behind the sums of the groups before theirs.  A workgroup
-// counts its whole group; a wavefront copies a token's entries at once, MV_HELD tokens of them under way.
-constexpr int MV_PART = 64, MV_HELD = 4;
-__global__ __launch_bounds__(MV_NT) void kvq_move_lists(MvArgs a, const int32_t *__restrict__ tokens, const uint32_t *__restrict__ sums)
+// Pointers and entries of MV_PART listed tokens on one side, behind the sums of the groups before theirs.  A workgroup counts its whole
+// group; a wavefront copies a token's entries at once, MV_HELD tokens of them under way.
+constexpr int MV_PART = 64, MV_HELD = 4, MV_LIST_WGS = 2 * MV_GROUP / MV_PART;          // workgroups of a group
+struct MvListShared {
+    uint32_t wave_sum[2][MV_NT / 64], begin[MV_GROUP + 1], from[MV_GROUP];
+};
+__device__ void mv_list_part(const MvJob &j, const int32_t *__restrict__ tokens, const uint32_t *__restrict__ sums, int wg, int side, int quarter,
+                             MvListShared &sh)
 {
-    __shared__ uint32_t wave_sum[2][MV_NT / 64], begin[MV_GROUP + 1], from[MV_GROUP];
-    const MvJob &j = a.job[0];
+    auto &wave_sum = sh.wave_sum;
+    auto &begin = sh.begin;
+    auto &from = sh.from;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int side = blockIdx.x & 1, quarter = (blockIdx.x >> 1) & 3, wg = blockIdx.x >> 3;
     const MvSide &s = side == 0 ? j.k : j.v;
     const uint32_t room = side == 0 ? j.k_room : j.v_room;
     const int i0 = wg * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
@@ -337,6 +309,49 @@ __global__ __launch_bounds__(MV_NT) void kvq_move_lists(MvArgs a, const int32_t 
     }
 }
 
+// The kernel of a copy, and the second of a gather (LIST).
+template <int BITS, bool LIST>
+__global__ __launch_bounds__(MV_NT) void kvq_move(MvArgs a, const int32_t *__restrict__ tokens, const uint32_t *__restrict__ sums)
+{
+    int wg = blockIdx.x, i = 0;
+    if (!LIST) {                                            // (a gather is one job: a fixed place in the arguments)
+        while (i + 1 < a.n_jobs && wg >= a.wg0[i + 1]) ++i;
+        wg -= a.wg0[i];
+    }
+    const MvJob &j = a.job[LIST ? 0 : i];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = LIST ? MV_LIST_WGS : 2, groups = mv_groups(j.n) * per;
+    if (wg < groups) {
+        const int i0 = wg / per * MV_GROUP, n = j.n - i0 < MV_GROUP ? j.n - i0 : MV_GROUP;
+        if (wg % per == 1) mv_scales<LIST>(j, tokens, a.heads, i0, n);
+        if constexpr (LIST) {
+            __shared__ MvListShared sh;
+            mv_list_part(j, tokens, sums, wg / per, wg & 1, (wg % per) >> 1, sh);
+        } else {
+            mv_run_side((wg & 1) ? j.v : j.k, (wg & 1) ? j.v_room : j.k_room, j.s_shift, j.d_shift, j.first + i0, j.at + i0, j.at, j.first, n, j.status);
+        }
+        return;
+    }
+    wg -= groups;
+    if (j.s_params) {
+        const int wgs = (a.param_words + 16 * MV_NT - 1) / (16 * MV_NT);
+        if (wg < wgs) {
+            for (int w = wg * 16 * MV_NT + tid; w < a.param_words && w < (wg + 1) * 16 * MV_NT; w += MV_NT) j.d_params[w] = j.s_params[w];
+            return;
+        }
+        wg -= wgs;
+    }
+    const int key_items = mv_key_items(j.at, j.n) * a.heads, value_items = 2 * mv_value_items(j.at, j.n) * a.heads;
+    const int key_wgs = (key_items + 3) / 4;
+    if (wg < key_wgs) {
+        const int item = wg * 4 + wave;
+        if (item < key_items) mv_keys<BITS, LIST>(j, tokens, item, lane);
+    } else {
+        const int item = (wg - key_wgs) * 4 + wave;
+        if (item < value_items) mv_values<BITS, LIST>(j, tokens, item, lane);
+    }
+}
+
 // Whether tokens may go from `src` to `dst`.
 kvq_status mv_check(const kvq_cache *dst, const kvq_cache *src, int64_t n)
 {
@@ -384,11 +399,11 @@ void mv_job(MvJob &j, const kvq_cache *dst, const kvq_cache *src, int64_t first,
 int64_t mv_wgs(const MvJob &j, int heads, int param_words, bool list)
 {
     const int64_t keys = (int64_t)mv_key_items(j.at, j.n) * heads, values = 2 * (int64_t)mv_value_items(j.at, j.n) * heads;
-    return mv_groups(j.n) * (list ? 1 : 2) + (j.s_params ? (param_words + 16 * MV_NT - 1) / (16 * MV_NT) : 0) + (keys + 3) / 4 + (values + 3) / 4;
+    return mv_groups(j.n) * (list ? MV_LIST_WGS : 2) + (j.s_params ? (param_words + 16 * MV_NT - 1) / (16 * MV_NT) : 0) + (keys + 3) / 4 + (values + 3) / 4;
 }
 
 template <bool LIST>
-kvq_status mv_launch(const MvArgs &a, int bits, int64_t wgs, const int32_t *tokens, uint32_t *sums, hipStream_t s)
+kvq_status mv_launch(const MvArgs &a, int bits, int64_t wgs, const int32_t *tokens, const uint32_t *sums, hipStream_t s)
 {
     const dim3 grid((unsigned)wgs), block(MV_NT);
     if (bits == 2) kvq_move<2, LIST><<<grid, block, 0, s>>>(a, tokens, sums);
@@ -469,10 +484,11 @@ extern "C" kvq_status kvq_cache_gather(kvq_cache *dst, const kvq_cache *src, con
     const int64_t wgs = mv_wgs(a.job[0], a.heads, a.param_words, true);
     a.wg0[1] = (int32_t)wgs;
     if (wgs >= ((int64_t)1 << 31)) return KVQ_ERR_UNSUPPORTED;
-    const kvq_status go = mv_launch<true>(a, dst->bits, wgs, d_tokens, (uint32_t *)dst->workspace, (hipStream_t)stream);
-    if (go != KVQ_OK) return go;
-    kvq_move_lists<<<dim3((unsigned)(8 * groups)), dim3(MV_NT), 0, (hipStream_t)stream>>>(a, d_tokens, (const uint32_t *)dst->workspace);
+    uint32_t *sums = (uint32_t *)dst->workspace;
+    kvq_move_counts<<<dim3((unsigned)groups), dim3(MV_NT), 0, (hipStream_t)stream>>>(a.job[0], d_tokens, sums);
     KVQ_HIP_CHECK(hipGetLastError());
+    const kvq_status go = mv_launch<true>(a, dst->bits, wgs, d_tokens, sums, (hipStream_t)stream);
+    if (go != KVQ_OK) return go;
     mv_done(dst, src, n);
     return KVQ_OK;
 }
