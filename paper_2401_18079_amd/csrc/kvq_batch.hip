@@ -418,23 +418,44 @@ struct BtConst {
     __attribute__((aligned(16))) uint32_t s[64], z[64];    // Key scales and zero-points: (channel i, channel i + 64) fp16
     __attribute__((aligned(16))) float vh[64];             // theta_i / 2 pi
     float red[BT_WAVES];
-    __device__ void stage(const BtArgs &a, const BtSeg &sg, const BtPart &p)
+    // What a thread brings along: requested together, put into LDS when the other requests of the start are under way as well.
+    struct Brought {
+        float k0, k1, v0, v1, vh, m;
+        uint16_t s0, s1, z0, z1;
+    };
+    static __device__ __forceinline__ Brought load(const BtArgs &a, const BtSeg &sg, const BtPart &p)
+    {
+        static_assert(NE * NE <= BT_NT, "a field per thread");
+        const int tid = threadIdx.x, f = tid & (NE * NE - 1), c = p.h * 128 + (tid & 63), b = p.b0 + tid;
+        const KvqParamsView pv = kvq_params_view(sg.params, a.heads * KVQ_HEAD_DIM);
+        Brought t;
+        t.k0 = pv.hdr->lut_k[f & (NE - 1)];
+        t.k1 = pv.hdr->lut_k[f >> BITS];
+        t.v0 = pv.hdr->lut_v[f & (NE - 1)];
+        t.v1 = pv.hdr->lut_v[f >> BITS];
+        t.s0 = pv.s16[c];
+        t.s1 = pv.s16[c + 64];
+        t.z0 = pv.z16[c];
+        t.z1 = pv.z16[c + 64];
+        t.vh = pv.hdr->rope_vh[tid & 63];
+        t.m = a.w.smax[sg.blk0 + (b < p.b1 ? b : p.b1 - 1)];
+        return t;
+    }
+    __device__ __forceinline__ void stage(const BtArgs &a, const BtSeg &sg, const BtPart &p, const Brought &t)
     {
         const int tid = threadIdx.x;
-        const KvqParamsView pv = kvq_params_view(sg.params, a.heads * KVQ_HEAD_DIM);
-        for (int f = tid; f < NE * NE; f += BT_NT) {
-            const half2_t k = {(_Float16)pv.hdr->lut_k[f & (NE - 1)], (_Float16)pv.hdr->lut_k[f >> BITS]};
-            const half2_t v = {(_Float16)pv.hdr->lut_v[f & (NE - 1)], (_Float16)pv.hdr->lut_v[f >> BITS]};
-            lut_k[f] = __builtin_bit_cast(uint32_t, k);
-            lut_v[f] = __builtin_bit_cast(uint32_t, v);
+        if (tid < NE * NE) {
+            const half2_t k = {(_Float16)t.k0, (_Float16)t.k1}, v = {(_Float16)t.v0, (_Float16)t.v1};
+            lut_k[tid] = __builtin_bit_cast(uint32_t, k);
+            lut_v[tid] = __builtin_bit_cast(uint32_t, v);
         }
         if (tid < 64) {
-            s[tid] = pv.s16[p.h * 128 + tid] | ((uint32_t)pv.s16[p.h * 128 + 64 + tid] << 16);
-            z[tid] = pv.z16[p.h * 128 + tid] | ((uint32_t)pv.z16[p.h * 128 + 64 + tid] << 16);
-            vh[tid] = pv.hdr->rope_vh[tid];
+            s[tid] = t.s0 | ((uint32_t)t.s1 << 16);
+            z[tid] = t.z0 | ((uint32_t)t.z1 << 16);
+            vh[tid] = t.vh;
         }
-        float m = 0.0f;
-        for (int b = p.b0 + tid; b < p.b1; b += BT_NT) m = __builtin_fmaxf(m, a.w.smax[sg.blk0 + b]);
+        float m = t.m;
+        for (int b = p.b0 + tid + BT_NT; b < p.b1; b += BT_NT) m = __builtin_fmaxf(m, a.w.smax[sg.blk0 + b]);
         m = kvq_wave_max(m);
         if ((tid & 63) == 0) red[tid >> 6] = m;
     }
@@ -687,6 +708,7 @@ template <int BITS, int MB, int WHICH>
 struct BtAlone {
     static constexpr int PER_CU = MB == 1 ? 3 : 2;
     static constexpr int QBYTES = 8192 * MB, PATCHES = BT_WAVES * BT_PATCH;
+    static_assert(QBYTES == 2 * MB * BT_NT * 16, "two pieces of a block's rows per thread");
     static_assert(16 * 128 * 4 == BT_PATCH, "the sums of 16 queries take a patch's place");
     struct Shared {
         __attribute__((aligned(16))) uint8_t area[PATCHES], qfrag[QBYTES];
@@ -741,16 +763,16 @@ __device__ __forceinline__ void BtAlone<BITS, MB, WHICH>::run(const BtArgs &a, i
         vc[0].load(v_plane, n0, my);
         vc[1].load(v_plane + v_half, n0, my);
     }
-    con.stage(a, sg, p);
+    // Everything else the start reads, before anything of it is waited for; the lists' entries behind their places.
+    const typename BtConst<BITS>::Brought brought = BtConst<BITS>::load(a, sg, p);
+    uint4 rows[2 * MB];
 #pragma unroll
-    for (int i = tid; i < QBYTES / 16; i += BT_NT) {
-        const int l = i & 63, t = (i >> 6) & 3, part = (i >> 8) & 1, mb = i >> 9;
+    for (int k = 0; k < 2 * MB; ++k) {
+        const int i = tid + k * BT_NT, l = i & 63, t = (i >> 6) & 3, part = (i >> 8) & 1, mb = i >> 9;
         const int row = (p.qb * MB + mb) * 16 + (l & 15);
-        uint4 v = {0u, 0u, 0u, 0u};
-        if (row < p.n_q) v = *(const uint4 *)(a.w.rows[WHICH] + (p.row0 + row) * BT_ROW + part * 128 + (t * 4 + (l >> 4)) * 8);
-        *(uint4 *)(qfrag + i * 16) = v;
+        rows[k] = uint4{0u, 0u, 0u, 0u};
+        if (row < p.n_q) rows[k] = *(const uint4 *)(a.w.rows[WHICH] + (p.row0 + row) * BT_ROW + part * 128 + (t * 4 + (l >> 4)) * 8);
     }
-    for (int i = tid; i < PATCHES / 16; i += BT_NT) *(uint4 *)(area + i * 16) = uint4{0u, 0u, 0u, 0u};
     const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
     const float my_vh = hdr->rope_vh[lane], my_vl = hdr->rope_vl[lane];
     BtSums<MB> sum;
@@ -763,6 +785,10 @@ __device__ __forceinline__ void BtAlone<BITS, MB, WHICH>::run(const BtArgs &a, i
     BtPlaces at(tab, 0);
     if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
     if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
+    for (int i = tid; i < PATCHES / 16; i += BT_NT) *(uint4 *)(area + i * 16) = uint4{0u, 0u, 0u, 0u};
+    con.stage(a, sg, p, brought);
+#pragma unroll
+    for (int k = 0; k < 2 * MB; ++k) *(uint4 *)(qfrag + (tid + k * BT_NT) * 16) = rows[k];
     __syncthreads();
     const float kap = con.kappa();
     float minus_one = -1.0f, one = 1.0f;
@@ -930,8 +956,7 @@ __device__ __forceinline__ void BtTogether<BITS, QW, WHICH>::run(const BtArgs &a
     const BtSeg sg = bt_seg(a.w.segs[p.si]);
     uint8_t *const patches = keys + KEYS, *const values = patches + 2 * BT_PATCH;
 
-    con.stage(a, sg, p);
-    for (int i = tid; i < 2 * BT_PATCH / 16; i += BT_NT) *(uint4 *)(patches + i * 16) = uint4{0u, 0u, 0u, 0u};
+    const typename BtConst<BITS>::Brought brought = BtConst<BITS>::load(a, sg, p);
     const int q0 = (p.qb * QW + qg) * 32;
     half8_t qf[MB][4][2];
     BtSums<MB> sum;
@@ -952,10 +977,6 @@ __device__ __forceinline__ void BtTogether<BITS, QW, WHICH>::run(const BtArgs &a
     }
     const KvqParamsHeader *hdr = (const KvqParamsHeader *)sg.params;
     const float my_vh = hdr->rope_vh[lane], my_vl = hdr->rope_vl[lane];
-    __syncthreads();
-    const float kap = con.kappa();
-    float minus_one = -1.0f;
-    asm("" : "+v"(minus_one));
     const uint8_t *const k_plane = sg.k_codes + (int64_t)sg.cap * 16 * BITS * p.h, *const v_plane = sg.v_codes + (int64_t)sg.cap * 16 * BITS * p.h;
     const int64_t v_half = (int64_t)(sg.cap >> 1) * 16 * BITS;
     const BtLane<BITS> my(r16, g);
@@ -986,6 +1007,12 @@ __device__ __forceinline__ void BtTogether<BITS, QW, WHICH>::run(const BtArgs &a
     for (int gr = 0; gr < 2; ++gr) vc[gr].load(my_half, block_of(0, gr) * BT_BLOCK, my);
     if (at.k0 + lane < at.k1) ke = k_list[at.k0 + lane];
     if (at.v0 + lane < at.v1) ve = v_list[at.v0 + lane];
+    for (int i = tid; i < 2 * BT_PATCH / 16; i += BT_NT) *(uint4 *)(patches + i * 16) = uint4{0u, 0u, 0u, 0u};
+    con.stage(a, sg, p, brought);
+    __syncthreads();
+    const float kap = con.kappa();
+    float minus_one = -1.0f;
+    asm("" : "+v"(minus_one));
     uint8_t *const my_keys = keys + wave * 8192;
     uint8_t *const my_patch = patches + mine * BT_PATCH;
 
