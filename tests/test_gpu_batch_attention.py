@@ -156,6 +156,37 @@ def test_batch_matches_the_definition(name, ov, prefix, own, sink, blocked):
         close(got, *reference(None, both(per, 0), q, SCALE, wl.rope_base))
 
 
+@pytest.mark.parametrize("heads,ratio,fraction,bits", [(16, 1, 0.01, 3), (17, 1, 0.01, 3), (17, 2, 0.3, 4), (64, 1, 0.05, 2), (80, 1, 0.01, 3)])
+def test_wide_layers(heads, ratio, fraction, bits):
+    """Outliers of a token over 16, 17, 64 and 80 heads: both sizes of the sort, more than one head a lane, lists read twice."""
+    wl = S.workload("c2", n_kv_heads=heads, n_q_heads=heads * ratio, outlier_fraction=fraction, bits=bits)
+    sq = Seqs(Setup(wl))
+    pre = sq.make(101)
+    per = [sq.make(n, seq=1 + n) for n in (3, 70)]
+    assert not compare_caches(*pre)
+    q = queries(wl, 2)
+    close(call(pre[1], both(per, 1), q), *reference(pre[0], both(per, 0), q, SCALE, wl.rope_base))
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its workspace, over the same caches."""
+    import torch
+    import paper_2401_18079_amd as K
+    wl = S.workload("c2", n_kv_heads=4, n_q_heads=8)
+    sq = Seqs(Setup(wl))
+    pre, per = sq.make(700), [sq.make(20 + i, seq=1 + i) for i in range(3)]
+    q = [torch.from_numpy(queries(wl, 3, seed=s)).cuda() for s in range(2)]
+    ref = [call(pre[1], both(per, 1), x) for x in q]
+    outs = [[torch.zeros_like(ref[0]) for _ in range(8)] for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for j in range(2):
+            K.kvq_attention_decode_batch(pre[1], both(per, 1), q[j], SCALE, outs[j][i], stream=streams[j])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, ref[j]) for j in range(2) for o in outs[j])
+
+
 def test_more_sequences_than_one_launch_describes():
     wl = S.workload("c2", n_kv_heads=2, n_q_heads=4)
     sq = Seqs(Setup(wl))
